@@ -378,6 +378,87 @@ int e0m4_int4_dequant(const void* codes, int64_t N, int64_t K, int group, void* 
 int e0m4_int4_gemv(const void* X_f16, const void* codes, int64_t N, int64_t K, int group, void* Y_f16, void* stream);
 
 /*
+ * A cache of keys and values in E0M4 codes, and the operators around it: new
+ * rows are quantised into it (append), attention reads it as it is, rows that
+ * received little attention leave it (evict), rows are read back (read).
+ *
+ *   - A cache holds `capacity` rows of keys and of values for each of `batch`
+ *     sequences and `kv_heads` heads, in an opaque layout of e0m4_kv4_bytes()
+ *     bytes.  It needs no initialisation.  dim is 64, 128 or 256; group (along
+ *     dim) 32, 64 or 128, at most dim; batch and kv_heads <= 65535, capacity <=
+ *     2^26, batch * kv_heads * capacity <= 2^40.
+ *   - A row is stored as e0m4_quantize stores a row of weights: per group a
+ *     scale and a bias, codes under the same map and rounding.  fp16 and bfloat16
+ *     rows alike get fp16 parameters; NaN is stored as 0 and magnitudes above
+ *     57344 as 57344, so every stored value is finite.  What a code stands for is
+ *     fp16((2 + code/8 - bias) * scale), in attention too.
+ *   - e0m4_kv4_rows is a view [batch, n, heads, dim] of rows: strides in
+ *     elements, dim contiguous, data 16-byte aligned and strides multiples of 8
+ *     (columns of a projection's output, for instance; a stride may be 0).
+ *   - lengths, starts, counts and first are int32 device arrays, one value per
+ *     sequence.  Lengths are taken as in [0, capacity], counts as in [0, n_new]
+ *     (NULL: n_new each).
+ * Errors, streams and empty problems are as elsewhere in this file.
+ */
+typedef struct { int64_t batch, kv_heads, capacity; int dim, group; } e0m4_kv4_shape;
+typedef struct { const void* data; int64_t batch_ld, row_ld, head_ld; } e0m4_kv4_rows;
+/* Truth values [batch, n_new, rows], one byte each, by strides in bytes (0 to
+ * share); rows of the cache from `rows` on are not seen. */
+typedef struct { const void* data; int64_t batch_ld, row_ld, rows; } e0m4_kv4_mask;
+#define E0M4_KV4_FP16 0
+#define E0M4_KV4_BF16 1
+
+size_t e0m4_kv4_bytes(const e0m4_kv4_shape* shape);
+
+/* Rows i < counts[b] of keys and values [batch, n_new, kv_heads, dim] become rows
+ * starts[b] + i of the cache; those outside [0, capacity) are skipped, other rows
+ * keep what they hold. */
+int e0m4_kv4_append(void* cache, const e0m4_kv4_shape* shape, const e0m4_kv4_rows* keys, const e0m4_kv4_rows* values,
+                    int dtype, int64_t n_new, const int32_t* starts, const int32_t* counts, void* stream);
+
+/* Rows first[b] + i, i < rows (first NULL: 0), as fp16 [batch, rows, kv_heads, dim];
+ * zeros outside [0, lengths[b]). */
+int e0m4_kv4_read(const void* cache, const e0m4_kv4_shape* shape, const int32_t* lengths, const int32_t* first, int64_t rows,
+                  void* keys_f16, void* values_f16, void* stream);
+
+/*
+ * Attention of queries [batch, n_new, heads, dim], the newest counts[b] of the
+ * lengths[b] rows of each sequence (already appended), over the cache:
+ *     out[b,i,h] = sum_j softmax_j(q[b,i,h] . k[b,j,g] / sqrt(dim)) v[b,j,g],
+ * g = h / (heads / kv_heads), over the rows j that query i sees: j < lengths[b];
+ * if `causal`, j <= p = lengths[b] - counts[b] + i; if window > 0 (causal only), j >
+ * p - window; if `mask`, those it has set.  A query that sees no row, and queries
+ * i >= counts[b], get zeros.  out is [batch, n_new, heads, dim] in the queries'
+ * type.  heads / kv_heads <= 1024, n_new <= 2^20, heads / kv_heads * n_new <= 2^24.
+ *   weights (NULL: none) is [batch, kv_heads, capacity] fp32; weights[b,g,j] +=
+ * the sum of row j's softmax weights over the queries and the heads of g, for j <
+ * lengths[b] (what lies behind is not touched).
+ * Scores, sums and products are accumulated in fp32, the softmax weights are
+ * rounded to fp16 for their product with the values; bfloat16 queries are used as
+ * fp16 after scaling each by a power of two.  Workspace as for e0m4_matmul
+ * (e0m4_kv4_attention_workspace_bytes bytes).  The result is deterministic.
+ */
+size_t e0m4_kv4_attention_workspace_bytes(const e0m4_kv4_shape* shape, int64_t heads, int64_t n_new, int with_weights);
+int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, int64_t n_new, const void* cache,
+                       const e0m4_kv4_shape* shape, const int32_t* lengths, const int32_t* counts, int causal, int64_t window,
+                       const e0m4_kv4_mask* mask, float* weights, void* out, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * Eviction: of each sequence and head with more than `budget` rows, the newest
+ * `recent` and the budget - recent others that received most stay (ties go to the
+ * lower row; NaN counts as the most), in their order; shorter ones stay whole.
+ * The rows that stay become the first rows of `small`, another cache of the same
+ * batch, heads, dim and group with capacity >= budget >= 1.
+ *   received is [batch, kv_heads, capacity] fp32.  kept [batch, kv_heads, budget]
+ * int32 gets their row numbers, received_out (same shape, fp32) what they received
+ * (-1 and 0 behind the last), lengths_out [batch] min(lengths[b], budget).
+ */
+int e0m4_kv4_evict(const void* cache, const e0m4_kv4_shape* shape, const float* received, const int32_t* lengths,
+                   int64_t budget, int64_t recent, void* small, const e0m4_kv4_shape* small_shape, int32_t* kept,
+                   int32_t* lengths_out, float* received_out, void* stream);
+
+/*
  * Diagnostics for tuning sweeps and for tests that force every kernel variant;
  * not needed for normal use.  Sets an integer knob by name (e.g. "gemv_waves");
  * unknown names return E0M4_ERR_SHAPE.  A value of 0 restores the built-in

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -17,6 +18,28 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libe0m4.so")
 
 _lib = None
+
+
+class E0M4KV4Shape(NamedTuple):
+    """Sizes of a key/value cache in E0M4 codes (see include/e0m4.h)."""
+    batch: int
+    kv_heads: int
+    capacity: int
+    dim: int
+    group: int
+
+
+class _KV4Shape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("capacity", ctypes.c_int64), ("dim", ctypes.c_int),
+                ("group", ctypes.c_int)]
+
+
+class _KV4Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_ld", ctypes.c_int64), ("row_ld", ctypes.c_int64), ("head_ld", ctypes.c_int64)]
+
+
+class _KV4Mask(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_ld", ctypes.c_int64), ("row_ld", ctypes.c_int64), ("rows", ctypes.c_int64)]
 
 
 class E0M4Error(RuntimeError):
@@ -88,6 +111,19 @@ def lib() -> ctypes.CDLL:
     L.e0m8_workspace_bytes.argtypes = [i64, i64, i64, ci]
     L.e0m4_kv_append.restype = ci
     L.e0m4_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp]
+    shp, rws, msk = ctypes.POINTER(_KV4Shape), ctypes.POINTER(_KV4Rows), ctypes.POINTER(_KV4Mask)
+    L.e0m4_kv4_bytes.restype = sz
+    L.e0m4_kv4_bytes.argtypes = [shp]
+    L.e0m4_kv4_append.restype = ci
+    L.e0m4_kv4_append.argtypes = [vp, shp, rws, rws, ci, i64, vp, vp, vp]
+    L.e0m4_kv4_read.restype = ci
+    L.e0m4_kv4_read.argtypes = [vp, shp, vp, vp, i64, vp, vp, vp]
+    L.e0m4_kv4_attention_workspace_bytes.restype = sz
+    L.e0m4_kv4_attention_workspace_bytes.argtypes = [shp, i64, i64, ci]
+    L.e0m4_kv4_attention.restype = ci
+    L.e0m4_kv4_attention.argtypes = [rws, ci, i64, i64, vp, shp, vp, vp, ci, i64, msk, vp, vp, vp, sz, vp]
+    L.e0m4_kv4_evict.restype = ci
+    L.e0m4_kv4_evict.argtypes = [vp, shp, vp, vp, i64, i64, vp, shp, vp, vp, vp, vp]
     L.e0m4_int4_quantize.restype = ci
     L.e0m4_int4_quantize.argtypes = [vp, i64, i64, ci, vp, vp, vp, vp]
     L.e0m4_int4_dequant.restype = ci
@@ -325,6 +361,127 @@ def e0m4_kv_append(cache, new_rows, position_ids, stream=None):
     _check(lib().e0m4_kv_append(_ptr(cache), max_seq, row, _ptr(new_rows), n_new, new_rows.stride(0),
                                 _ptr(position_ids), _stream(stream)), "e0m4_kv_append")
     return cache
+
+
+# ---- key/value cache in E0M4 codes (see include/e0m4.h) ----------------------------------------------
+
+_KV4_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _kv4_per_sequence(t, shape, name: str, where: str):
+    """Device int32 [batch], or None."""
+    if t is not None and (t.dtype != torch.int32 or t.shape != (shape.batch,) or not t.is_contiguous() or not t.is_cuda):
+        raise ValueError("%s: %s must be a contiguous cuda int32 tensor of shape (%d,), got %s %s on %s"
+                         % (where, name, shape.batch, t.dtype, tuple(t.shape), t.device))
+    return _ptr(t)
+
+
+def _kv4_rows(t, n: int, heads: int, shape, name: str, where: str):
+    """A [batch, n, heads, dim] tensor of any strides but the last."""
+    if t.dtype not in _KV4_DTYPES:
+        raise TypeError("%s: %s must be float16 or bfloat16" % (where, name))
+    if t.shape != (shape.batch, n, heads, shape.dim) or (t.numel() and t.stride(3) != 1) or not t.is_cuda:
+        raise ValueError("%s: %s must be a cuda tensor of shape %s whose last dimension is contiguous, got %s with strides %s on %s"
+                         % (where, name, (shape.batch, n, heads, shape.dim), tuple(t.shape), t.stride(), t.device))
+    # (the stride of a dimension of one is never walked, whatever it says)
+    ld = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+    return _KV4Rows(t.data_ptr(), *ld)
+
+
+def _kv4_cache(cache, shape, name: str, where: str):
+    need = e0m4_kv4_bytes(shape)
+    if cache.dtype != torch.uint8 or not cache.is_contiguous() or not cache.is_cuda or cache.numel() < need:
+        raise ValueError("%s: %s must be a contiguous cuda uint8 tensor of at least %d bytes" % (where, name, need))
+    return _KV4Shape(*shape)
+
+
+def e0m4_kv4_bytes(shape: E0M4KV4Shape) -> int:
+    return lib().e0m4_kv4_bytes(_KV4Shape(*shape))
+
+
+def e0m4_kv4_attention_workspace_bytes(shape: E0M4KV4Shape, heads: int, n_new: int, with_weights: bool = False) -> int:
+    return lib().e0m4_kv4_attention_workspace_bytes(_KV4Shape(*shape), heads, n_new, 1 if with_weights else 0)
+
+
+def e0m4_kv4_alloc(shape: E0M4KV4Shape, device) -> torch.Tensor:
+    """Memory for a cache (uninitialised: rows count once they are appended)."""
+    need = e0m4_kv4_bytes(shape)
+    if need == 0 and shape.batch * shape.kv_heads * shape.capacity != 0:
+        raise ValueError("e0m4_kv4_alloc: unsupported shape %s" % (shape,))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+
+
+def e0m4_kv4_append(cache, shape: E0M4KV4Shape, keys, values, starts, counts=None, stream=None):
+    """Rows of keys and values [batch, n, kv_heads, dim] (fp16 or bf16, any strides but the last) are quantised into the
+    cache from row starts[b] on, the first counts[b] of them (None: all)."""
+    where = "e0m4_kv4_append"
+    n = keys.shape[1]
+    k, v = (_kv4_rows(t, n, shape.kv_heads, shape, name, where) for t, name in ((keys, "keys"), (values, "values")))
+    if keys.dtype != values.dtype:
+        raise TypeError("e0m4_kv4_append: keys and values must be of one type")
+    _check(lib().e0m4_kv4_append(_ptr(cache), _kv4_cache(cache, shape, "cache", where), k, v, _KV4_DTYPES[keys.dtype], n,
+                                 _kv4_per_sequence(starts, shape, "starts", where), _kv4_per_sequence(counts, shape, "counts", where),
+                                 _stream(stream)), where)
+    return cache
+
+
+def e0m4_kv4_read(cache, shape: E0M4KV4Shape, lengths, rows: int, first=None, stream=None):
+    """(keys, values) fp16 [batch, rows, kv_heads, dim]: what the codes of rows first[b] + i stand for, zeros from lengths[b] on."""
+    where = "e0m4_kv4_read"
+    s = _kv4_cache(cache, shape, "cache", where)
+    size = (shape.batch, max(rows, 0), shape.kv_heads, shape.dim)
+    keys, values = (_empty(size, torch.float16, cache.device, stream, "cache's rows") for _ in range(2))
+    _check(lib().e0m4_kv4_read(_ptr(cache), s, _kv4_per_sequence(lengths, shape, "lengths", where),
+                               _kv4_per_sequence(first, shape, "first", where), rows, _ptr(keys), _ptr(values), _stream(stream)), where)
+    return keys, values
+
+
+def e0m4_kv4_attention(queries, cache, shape: E0M4KV4Shape, lengths, counts=None, causal: bool = True, window: int = 0, mask=None,
+                       weights=None, out=None, workspace=None, stream=None):
+    """Attention of the newest tokens' queries [batch, n, heads, dim] over the cache; see include/e0m4.h.  mask: bool
+    [batch, n, rows] (dimensions of one are shared), weights: fp32 [batch, kv_heads, capacity], added to in place."""
+    where = "e0m4_kv4_attention"
+    batch, n, heads, dim = queries.shape
+    q = _kv4_rows(queries, n, heads, shape, "queries", where)
+    s = _kv4_cache(cache, shape, "cache", where)
+    m = None
+    if mask is not None:
+        if mask.dtype != torch.bool or mask.dim() != 3 or mask.shape[0] not in (1, batch) or mask.shape[1] not in (1, n) or \
+                (mask.numel() and mask.stride(2) != 1 and mask.shape[2] != 1) or not mask.is_cuda:
+            raise ValueError("e0m4_kv4_attention: mask must be a cuda bool tensor [batch, n, rows] with its rows side by side")
+        m = _KV4Mask(_ptr(mask), *(mask.stride(i) if mask.shape[i] > 1 else 0 for i in range(2)), mask.shape[2])
+    if weights is not None:
+        _need(weights, torch.float32, (shape.batch, shape.kv_heads, shape.capacity), "weights")
+    if out is None:
+        out = _empty((batch, n, heads, dim), queries.dtype, queries.device, stream, "out")
+    else:
+        _need(out, queries.dtype, (batch, n, heads, dim), "out")
+    if workspace is None:
+        need = lib().e0m4_kv4_attention_workspace_bytes(s, heads, n, 0 if weights is None else 1)
+        if need > 0:
+            workspace = _empty(need, torch.uint8, queries.device, stream, "workspace")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().e0m4_kv4_attention(q, _KV4_DTYPES[queries.dtype], heads, n, _ptr(cache), s,
+                                    _kv4_per_sequence(lengths, shape, "lengths", where), _kv4_per_sequence(counts, shape, "counts", where),
+                                    1 if causal else 0, window, m, _ptr(weights), _ptr(out), _ptr(workspace), ws_bytes, _stream(stream)),
+           where)
+    return out
+
+
+def e0m4_kv4_evict(cache, shape: E0M4KV4Shape, received, lengths, budget: int, recent: int, small, small_shape: E0M4KV4Shape,
+                   stream=None):
+    """The rows that received most attention, and the newest `recent`, move to the cache `small`.  Returns (kept int32
+    [batch, kv_heads, budget], lengths int32 [batch], received fp32 [batch, kv_heads, budget]); see include/e0m4.h."""
+    where = "e0m4_kv4_evict"
+    s, o = _kv4_cache(cache, shape, "cache", where), _kv4_cache(small, small_shape, "small", where)
+    _need(received, torch.float32, (shape.batch, shape.kv_heads, shape.capacity), "received")
+    size = (shape.batch, shape.kv_heads, max(budget, 0))
+    kept = _empty(size, torch.int32, cache.device, stream, "kept")
+    lengths_out = _empty((shape.batch,), torch.int32, cache.device, stream, "lengths")
+    received_out = _empty(size, torch.float32, cache.device, stream, "received")
+    _check(lib().e0m4_kv4_evict(_ptr(cache), s, _ptr(received), _kv4_per_sequence(lengths, shape, "lengths", where), budget, recent,
+                                _ptr(small), o, _ptr(kept), _ptr(lengths_out), _ptr(received_out), _stream(stream)), where)
+    return kept, lengths_out, received_out
 
 
 # ---- E0M8, the 8-bit member of the family (see include/e0m4.h) ---------------------------------------

@@ -1,0 +1,202 @@
+// C entries of the key/value cache in E0M4 codes: argument checks and the choice of kernels.  Every check happens on the host before
+// anything is enqueued.
+#include "e0m4_host.h"
+#include "e0m4_kv4.h"
+
+namespace e0m4 {
+
+namespace {
+
+constexpr int64_t kMaxCapacity = (int64_t)1 << 26, kMaxNew = (int64_t)1 << 20, kMaxGrid = 65535, kMaxShare = 1 << 10;
+constexpr int64_t kMaxRows = (int64_t)1 << 40;             // of all sequences and heads
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int check_kv4(const e0m4_kv4_shape* s)
+{
+    if (!s) return E0M4_ERR_NULL;
+    if (s->batch < 0 || s->batch > kMaxGrid || s->kv_heads < 0 || s->kv_heads > kMaxGrid || s->capacity < 0 || s->capacity > kMaxCapacity)
+        return E0M4_ERR_SHAPE;
+    if (s->batch * s->kv_heads > kMaxRows / (s->capacity ? s->capacity : 1)) return E0M4_ERR_SHAPE;
+    if (s->dim != 64 && s->dim != 128 && s->dim != 256) return E0M4_ERR_SHAPE;
+    if ((s->group != 32 && s->group != 64 && s->group != 128) || s->group > s->dim) return E0M4_ERR_GROUP;
+    return E0M4_OK;
+}
+bool empty(const e0m4_kv4_shape& s) { return s.batch == 0 || s.kv_heads == 0 || s.capacity == 0; }
+
+// A view that the kernels read in 16-byte pieces.
+int check_rows(const e0m4_kv4_rows* r)
+{
+    if (!r || !r->data) return E0M4_ERR_NULL;
+    if (!aligned(r->data, 16)) return E0M4_ERR_ALIGN;
+    if (((r->batch_ld | r->row_ld | r->head_ld) & 7) != 0) return E0M4_ERR_ALIGN;
+    return E0M4_OK;
+}
+Kv4Rows view(const e0m4_kv4_rows& r) { return Kv4Rows{r.data, r.batch_ld, r.row_ld, r.head_ld}; }
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+// How an attention call runs: chunks of the cache, and what the workspace holds.
+struct Plan {
+    int chunk_tiles, chunks;
+    size_t out_bytes, stats_bytes, lse_bytes;
+    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes; }
+};
+Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool weights)
+{
+    Plan p;
+    const int64_t rows = heads / s.kv_heads * n_new, all = s.batch * s.kv_heads * rows, tiles = kv4_tiles(s.capacity);
+    const int64_t sets = s.batch * s.kv_heads * ((rows + 15) / 16);
+    int64_t chunk = tiles * sets / 2048;
+    if (chunk < 4) chunk = 4;
+    if (chunk > tiles) chunk = tiles;
+    p.chunk_tiles = (int)chunk;
+    p.chunks = (int)((tiles + chunk - 1) / chunk);
+    p.out_bytes = p.chunks > 1 ? (size_t)p.chunks * all * s.dim * 4 : 0;
+    p.stats_bytes = p.chunks > 1 ? round16((size_t)p.chunks * all * 8) : 0;
+    p.lse_bytes = weights ? round16((size_t)all * 4) : 0;
+    return p;
+}
+int check_attention(const e0m4_kv4_shape* s, int64_t heads, int64_t n_new)
+{
+    const int rc = check_kv4(s);
+    if (rc != E0M4_OK) return rc;
+    if (heads < 0 || n_new < 0 || n_new > kMaxNew) return E0M4_ERR_SHAPE;
+    if (s->kv_heads == 0 ? heads != 0 : heads % s->kv_heads != 0 || heads / s->kv_heads > kMaxShare || heads == 0) return E0M4_ERR_SHAPE;
+    if (s->kv_heads && (heads / s->kv_heads * n_new > (int64_t)1 << 24 || s->batch * heads * n_new > (int64_t)1 << 32)) return E0M4_ERR_SHAPE;
+    return E0M4_OK;
+}
+
+__global__ void kv4_zero_kernel(uint4* y, int64_t pieces)
+{
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < pieces) y[i] = uint4{0, 0, 0, 0};
+}
+int zero_fill(void* y, int64_t bytes, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv4_zero_kernel, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, stream, static_cast<uint4*>(y), bytes / 16);
+    return check_launch();
+}
+
+}  // namespace
+
+}  // namespace e0m4
+
+using namespace e0m4;
+
+extern "C" {
+
+size_t e0m4_kv4_bytes(const e0m4_kv4_shape* s)
+{
+    if (check_kv4(s) != E0M4_OK) return 0;
+    return (size_t)s->batch * s->kv_heads * kv4_tiles(s->capacity) * kv4_tile_bytes(s->dim, s->group);
+}
+
+int e0m4_kv4_append(void* cache, const e0m4_kv4_shape* s, const e0m4_kv4_rows* keys, const e0m4_kv4_rows* values, int dtype, int64_t n_new,
+                    const int32_t* starts, const int32_t* counts, void* stream)
+{
+    int rc = check_kv4(s);
+    if (rc != E0M4_OK) return rc;
+    if (n_new < 0 || n_new > kMaxCapacity || (dtype != E0M4_KV4_FP16 && dtype != E0M4_KV4_BF16)) return E0M4_ERR_SHAPE;
+    if (empty(*s) || n_new == 0) return E0M4_OK;
+    if (!cache || !starts) return E0M4_ERR_NULL;
+    if ((rc = check_rows(keys)) != E0M4_OK || (rc = check_rows(values)) != E0M4_OK) return rc;
+    if (!aligned(cache, 16) || !aligned(starts, 4) || !aligned(counts, 4)) return E0M4_ERR_ALIGN;
+    return launch_kv4_append(cache, *s, view(*keys), view(*values), dtype, n_new, starts, counts, (hipStream_t)stream);
+}
+
+int e0m4_kv4_read(const void* cache, const e0m4_kv4_shape* s, const int32_t* lengths, const int32_t* first, int64_t rows, void* keys_f16,
+                  void* values_f16, void* stream)
+{
+    const int rc = check_kv4(s);
+    if (rc != E0M4_OK) return rc;
+    if (rows < 0 || rows > kMaxCapacity) return E0M4_ERR_SHAPE;
+    if (s->batch == 0 || s->kv_heads == 0 || rows == 0) return E0M4_OK;
+    if ((!cache && s->capacity) || !lengths || !keys_f16 || !values_f16) return E0M4_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(lengths, 4) || !aligned(first, 4) || !aligned(keys_f16, 16) || !aligned(values_f16, 16))
+        return E0M4_ERR_ALIGN;
+    return launch_kv4_read(cache, *s, lengths, first, rows, keys_f16, values_f16, (hipStream_t)stream);
+}
+
+size_t e0m4_kv4_attention_workspace_bytes(const e0m4_kv4_shape* s, int64_t heads, int64_t n_new, int with_weights)
+{
+    if (check_attention(s, heads, n_new) != E0M4_OK || empty(*s) || n_new == 0) return 0;
+    return plan_attention(*s, heads, n_new, with_weights != 0).bytes();
+}
+
+int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, int64_t n_new, const void* cache, const e0m4_kv4_shape* s,
+                       const int32_t* lengths, const int32_t* counts, int causal, int64_t window, const e0m4_kv4_mask* mask, float* weights,
+                       void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = check_attention(s, heads, n_new);
+    if (rc != E0M4_OK) return rc;
+    if (dtype != E0M4_KV4_FP16 && dtype != E0M4_KV4_BF16) return E0M4_ERR_SHAPE;
+    if (window < 0 || (window > 0 && !causal)) return E0M4_ERR_SHAPE;
+    if (mask && (mask->rows < 0 || mask->rows > kMaxCapacity)) return E0M4_ERR_SHAPE;
+    if (s->batch == 0 || s->kv_heads == 0 || n_new == 0) return E0M4_OK;
+    if (!out) return E0M4_ERR_NULL;
+    if (!aligned(out, 16)) return E0M4_ERR_ALIGN;
+    if (s->capacity == 0) return zero_fill(out, s->batch * n_new * heads * s->dim * 2, (hipStream_t)stream);
+    if (!cache || !lengths || (mask && !mask->data && mask->rows)) return E0M4_ERR_NULL;
+    if ((rc = check_rows(queries)) != E0M4_OK) return rc;
+    if (!aligned(cache, 16) || !aligned(lengths, 4) || !aligned(counts, 4) || !aligned(weights, 4)) return E0M4_ERR_ALIGN;
+    const Plan p = plan_attention(*s, heads, n_new, weights != nullptr);
+    if (p.bytes() > 0) {
+        if (!workspace) return E0M4_ERR_NULL;
+        if (!aligned(workspace, 16)) return E0M4_ERR_ALIGN;
+        if (workspace_bytes < p.bytes()) return E0M4_ERR_WORKSPACE;
+    }
+    Kv4Attention a = {};
+    a.cache = static_cast<const uint8_t*>(cache);
+    a.tiles = kv4_tiles(s->capacity);
+    a.q = view(*queries);
+    a.out = out;
+    a.lengths = lengths;
+    a.counts = counts;
+    if (mask) {
+        static const uint8_t none = 0;                  // (never read: the mask has no rows then)
+        a.mask = mask->data ? static_cast<const uint8_t*>(mask->data) : &none;
+        a.mask_batch_ld = mask->batch_ld;
+        a.mask_row_ld = mask->row_ld;
+        a.mask_rows = (int)mask->rows;
+    }
+    a.batch = (int)s->batch;
+    a.kv_heads = (int)s->kv_heads;
+    a.share = (int)(heads / s->kv_heads);
+    a.n_new = (int)n_new;
+    a.capacity = (int)s->capacity;
+    a.window = window < s->capacity ? (int)window : 0;  // (one that is never left is none)
+    a.causal = causal != 0;
+    a.bf16 = dtype == E0M4_KV4_BF16;
+    a.chunk_tiles = p.chunk_tiles;
+    a.chunks = p.chunks;
+    a.tile_rows = 16;
+    char* w = static_cast<char*>(workspace);
+    a.part_out = reinterpret_cast<float*>(w);
+    a.part_stats = reinterpret_cast<float2*>(w + p.out_bytes);
+    a.lse = weights ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes) : nullptr;
+    rc = launch_kv4_decode(a, *s, (hipStream_t)stream);
+    if (rc == E0M4_OK && a.chunks > 1) rc = launch_kv4_combine(a, *s, (hipStream_t)stream);
+    if (rc == E0M4_OK && weights) rc = launch_kv4_received(a, *s, weights, (hipStream_t)stream);
+    return rc;
+}
+
+int e0m4_kv4_evict(const void* cache, const e0m4_kv4_shape* s, const float* received, const int32_t* lengths, int64_t budget, int64_t recent,
+                   void* small, const e0m4_kv4_shape* o, int32_t* kept, int32_t* lengths_out, float* received_out, void* stream)
+{
+    int rc = check_kv4(s);
+    if (rc != E0M4_OK || (rc = check_kv4(o)) != E0M4_OK) return rc;
+    if (o->batch != s->batch || o->kv_heads != s->kv_heads || o->dim != s->dim || o->group != s->group) return E0M4_ERR_SHAPE;
+    if (budget < 1 || budget > o->capacity || recent < 0 || recent > budget) return E0M4_ERR_SHAPE;
+    if (s->batch == 0 || s->kv_heads == 0) return E0M4_OK;
+    if (!small || !lengths || !kept || !lengths_out || !received_out || ((!cache || !received) && s->capacity)) return E0M4_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(small, 16) || !aligned(received, 4) || !aligned(lengths, 4) || !aligned(kept, 4) ||
+        !aligned(lengths_out, 4) || !aligned(received_out, 4))
+        return E0M4_ERR_ALIGN;
+    const uintptr_t c0 = reinterpret_cast<uintptr_t>(cache), c1 = reinterpret_cast<uintptr_t>(small);
+    if (c0 < c1 + e0m4_kv4_bytes(o) && c1 < c0 + e0m4_kv4_bytes(s)) return E0M4_ERR_SHAPE;     // rows move while others are read
+    return launch_kv4_evict(cache, *s, received, lengths, (int)budget, (int)recent, small, *o, kept, lengths_out, received_out,
+                            (hipStream_t)stream);
+}
+
+}  // extern "C"

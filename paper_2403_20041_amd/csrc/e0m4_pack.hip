@@ -6,37 +6,15 @@
 // IEEE operation (divide, add, compare, convert), which is what makes the
 // codes reproducible bit for bit on another machine.
 #include "e0m4_device.h"
+#include "e0m4_encode.h"
 #include "e0m4_host.h"
 
 namespace e0m4 {
 
 namespace {
 
-constexpr float kLo = 2.0f;             // 2^n with n = 1
-constexpr float kHi = 3.998046875f;     // 2^(n+1) - eps, eps = one fp16 ulp of the binade (bits 0x43FF)
-constexpr float kSpan = 1.998046875f;   // kHi - kLo, exact
-constexpr float kMinScale = 6.103515625e-05f;   // smallest normal fp16
-constexpr float kMaxScale = 65504.0f;           // largest finite fp16
-
 constexpr int kThreads = 256;
 constexpr int kTileRows = 64;           // one workgroup handles 4 row blocks x 1 k block
-
-__device__ inline uint16_t half_bits(half_t h) { return __builtin_bit_cast(uint16_t, h); }
-__device__ inline half_t bits_half(uint16_t b) { return __builtin_bit_cast(half_t, b); }
-
-// code = min(y1 + y2, 15): y1 = four highest fraction bits of the mapped fp16
-// value, y2 = the bit below them (paper: quantization paragraph).
-// (y1 + y2 is the five bits above bit 5, plus one, halved; every value here lies in [2, 4))
-__device__ inline uint32_t encode_value(float w0, const Divisor& sf, float bf)
-{
-    float q = quotient(w0, sf);
-    float t = q + bf;
-    t = t < kLo ? kLo : t;
-    t = t > kHi ? kHi : t;
-    const uint32_t bits = half_bits((half_t)t);
-    const uint32_t c = (((bits >> 5) & 31u) + 1u) >> 1;
-    return c > 15u ? 15u : c;
-}
 
 // INT4 comparison format (paper: section "Evaluation of FP4 quantization"): q = clamp(rne(w / scale)
 // + zero, 0, 15) with an integer zero point kept as an fp16 number.
