@@ -429,7 +429,7 @@ int e0m4_kv4_read(const void* cache, const e0m4_kv4_shape* shape, const int32_t*
  * if `causal`, j <= p = lengths[b] - counts[b] + i; if window > 0 (causal only), j >
  * p - window; if `mask`, those it has set.  A query that sees no row, and queries
  * i >= counts[b], get zeros.  out is [batch, n_new, heads, dim] in the queries'
- * type.  heads / kv_heads <= 1024, n_new <= 2^20, heads / kv_heads * n_new <= 2^24.
+ * type.  heads / kv_heads <= 1024, n_new <= 2^20, heads / kv_heads * n_new <= 2^22.
  *   weights (NULL: none) is [batch, kv_heads, capacity] fp32; weights[b,g,j] +=
  * the sum of row j's softmax weights over the queries and the heads of g, for j <
  * lengths[b] (what lies behind is not touched).

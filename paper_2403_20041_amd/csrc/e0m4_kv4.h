@@ -130,17 +130,22 @@ struct Kv4Attention {
     const int* counts;                                  // or null: n_new each
     const uint8_t* mask;                                // or null; [batch, n_new, mask_rows] by its strides
     int64_t mask_batch_ld, mask_row_ld;
-    int mask_rows;
+    int mask_rows, mask_words;                          // (its runs of four rows can be read as words)
     int batch, kv_heads, share, n_new;
+    uint32_t share_inverse;                             // 2^32 / share rounded up, 0 for 1: exact for the 2^22 rows that there may be
     int capacity, window;                               // window 0: none
     int causal, bf16;
-    // Rows of the cache are dealt out in chunks of chunk_tiles tiles; with more than one, partial results meet in the workspace.
+    // Rows of the cache are dealt out in chunks of chunk_tiles tiles of tile_keys rows; with more than one chunk, partial results
+    // meet in the workspace.
     int chunk_tiles, chunks;
-    int tile_rows;                                      // rows of queries that go through the cache together
+    int tile_rows, tile_keys;                           // rows of queries that go through the cache together, rows of it at a time
     float* part_out;                                    // [chunk][batch][kv_heads][rows][dim]
     float2* part_stats;                                 // [chunk][batch][kv_heads][rows]: reference exponent, sum
     float* lse;                                         // [batch][kv_heads][rows] log2 of the softmax's sum, for the received weights
+    float* scores;                                      // [batch][kv_heads][rows][tiles * 32] in powers of two, or null
 };
+
+__device__ inline int kv4_query_of(const Kv4Attention& a, int row) { return a.share_inverse ? (int)__umulhi((uint32_t)row, a.share_inverse) : row; }
 
 // What a tile of `n` rows of queries, the first one `row0`, looks at.
 struct Kv4Span {
@@ -152,8 +157,8 @@ __device__ inline Kv4Span kv4_span(const Kv4Attention& a, int b, int row0, int n
     Kv4Span s;
     s.length = clamp_count(a.lengths[b], a.capacity);
     s.count = a.counts ? clamp_count(a.counts[b], a.n_new) : a.n_new;
-    const int i0 = row0 / a.share;
-    int i1 = (row0 + n - 1) / a.share;
+    const int i0 = kv4_query_of(a, row0);
+    int i1 = kv4_query_of(a, row0 + n - 1);
     i1 = i1 < s.count ? i1 : s.count - 1;
     s.begin = 0;
     s.end = s.length;
@@ -194,8 +199,14 @@ int launch_kv4_read(const void* cache, const e0m4_kv4_shape& s, const int* lengt
 int launch_kv4_evict(const void* cache, const e0m4_kv4_shape& s, const float* received, const int* lengths, int budget, int recent,
                      void* small, const e0m4_kv4_shape& o, int* kept, int* lengths_out, float* received_out, hipStream_t stream);
 // Attention: rows of queries in tiles of 16, a wavefront's tiles of the cache by itself; then, with several chunks, their sum.
+constexpr int kKv4ShortTiles = 32;      // caches of so many tiles are one workgroup's
 int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream);
-int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream);
+// ... in workgroups of a.tile_rows rows (128; with dim 128 also 256), which share the dequantised rows of the cache.
+constexpr int kKv4PrefillKeys = 64;
+int launch_kv4_prefill(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream);
+constexpr int kKv4MaxChunks = 2048;
+// (received, unless null: the rows' weights from the scores, in the same launch)
+int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream);
 // received[j] += the weights of row j, from the rows' log2 sums
 int launch_kv4_received(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream);
 

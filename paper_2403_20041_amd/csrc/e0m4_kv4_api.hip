@@ -36,25 +36,42 @@ Kv4Rows view(const e0m4_kv4_rows& r) { return Kv4Rows{r.data, r.batch_ld, r.row_
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// How an attention call runs: chunks of the cache, and what the workspace holds.
+// How an attention call runs: the kernel, chunks of the cache, and what the workspace holds.
 struct Plan {
-    int chunk_tiles, chunks;
-    size_t out_bytes, stats_bytes, lse_bytes;
-    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes; }
+    bool prefill, scores;
+    int tile_rows, tile_keys, chunk_tiles, chunks;
+    size_t out_bytes, stats_bytes, lse_bytes, scores_bytes;
+    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes + scores_bytes; }
 };
 Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool weights)
 {
     Plan p;
-    const int64_t rows = heads / s.kv_heads * n_new, all = s.batch * s.kv_heads * rows, tiles = kv4_tiles(s.capacity);
-    const int64_t sets = s.batch * s.kv_heads * ((rows + 15) / 16);
-    int64_t chunk = tiles * sets / 2048;
+    const int64_t rows = heads / s.kv_heads * n_new, all = s.batch * s.kv_heads * rows;
+    const int force = knob(Knob::kv4_attention);
+    p.prefill = force ? force >= 2 : rows > 32;
+    p.tile_keys = p.prefill ? kKv4PrefillKeys : kKv4Rows;
+    const int64_t tiles = (s.capacity + p.tile_keys - 1) / p.tile_keys;
+    auto sets = [&](int tile_rows) { return s.batch * s.kv_heads * ((rows + tile_rows - 1) / tile_rows); };
+    int64_t chunk;
+    if (p.prefill) {
+        p.tile_rows = s.dim == 128 && (force ? force == 3 : sets(256) >= 256 && 2 * n_new <= s.capacity) ? 256 : 128;
+        const int64_t n = sets(p.tile_rows);
+        chunk = n > 128 ? tiles : (tiles + 256 / n - 1) / (256 / n);
+    } else {
+        p.tile_rows = 16;
+        chunk = tiles * sets(16) / 2048;
+        if (tiles <= kKv4ShortTiles) chunk = tiles;
+    }
     if (chunk < 4) chunk = 4;
+    if (chunk < (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks) chunk = (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks;
     if (chunk > tiles) chunk = tiles;
     p.chunk_tiles = (int)chunk;
     p.chunks = (int)((tiles + chunk - 1) / chunk);
+    p.scores = weights && !p.prefill && rows <= 16;
     p.out_bytes = p.chunks > 1 ? (size_t)p.chunks * all * s.dim * 4 : 0;
     p.stats_bytes = p.chunks > 1 ? round16((size_t)p.chunks * all * 8) : 0;
     p.lse_bytes = weights ? round16((size_t)all * 4) : 0;
+    p.scores_bytes = p.scores ? (size_t)all * kv4_tiles(s.capacity) * kKv4Rows * 4 : 0;
     return p;
 }
 int check_attention(const e0m4_kv4_shape* s, int64_t heads, int64_t n_new)
@@ -63,7 +80,7 @@ int check_attention(const e0m4_kv4_shape* s, int64_t heads, int64_t n_new)
     if (rc != E0M4_OK) return rc;
     if (heads < 0 || n_new < 0 || n_new > kMaxNew) return E0M4_ERR_SHAPE;
     if (s->kv_heads == 0 ? heads != 0 : heads % s->kv_heads != 0 || heads / s->kv_heads > kMaxShare || heads == 0) return E0M4_ERR_SHAPE;
-    if (s->kv_heads && (heads / s->kv_heads * n_new > (int64_t)1 << 24 || s->batch * heads * n_new > (int64_t)1 << 32)) return E0M4_ERR_SHAPE;
+    if (s->kv_heads && (heads / s->kv_heads * n_new > (int64_t)1 << 22 || s->batch * heads * n_new > (int64_t)1 << 32)) return E0M4_ERR_SHAPE;
     return E0M4_OK;
 }
 
@@ -153,31 +170,36 @@ int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, i
     a.out = out;
     a.lengths = lengths;
     a.counts = counts;
-    if (mask) {
-        static const uint8_t none = 0;                  // (never read: the mask has no rows then)
-        a.mask = mask->data ? static_cast<const uint8_t*>(mask->data) : &none;
+    if (mask && mask->rows == 0) {                      // nothing is seen; any memory does for the address
+        a.mask = static_cast<const uint8_t*>(cache);
+    } else if (mask) {
+        a.mask = static_cast<const uint8_t*>(mask->data);
         a.mask_batch_ld = mask->batch_ld;
         a.mask_row_ld = mask->row_ld;
         a.mask_rows = (int)mask->rows;
+        a.mask_words = aligned(a.mask, 4) && ((mask->batch_ld | mask->row_ld | mask->rows) & 3) == 0;
     }
     a.batch = (int)s->batch;
     a.kv_heads = (int)s->kv_heads;
     a.share = (int)(heads / s->kv_heads);
     a.n_new = (int)n_new;
+    a.share_inverse = a.share > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.share - 1) / a.share) : 0;
     a.capacity = (int)s->capacity;
     a.window = window < s->capacity ? (int)window : 0;  // (one that is never left is none)
     a.causal = causal != 0;
     a.bf16 = dtype == E0M4_KV4_BF16;
     a.chunk_tiles = p.chunk_tiles;
     a.chunks = p.chunks;
-    a.tile_rows = 16;
+    a.tile_rows = p.tile_rows;
+    a.tile_keys = p.tile_keys;
     char* w = static_cast<char*>(workspace);
     a.part_out = reinterpret_cast<float*>(w);
     a.part_stats = reinterpret_cast<float2*>(w + p.out_bytes);
     a.lse = weights ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes) : nullptr;
-    rc = launch_kv4_decode(a, *s, (hipStream_t)stream);
-    if (rc == E0M4_OK && a.chunks > 1) rc = launch_kv4_combine(a, *s, (hipStream_t)stream);
-    if (rc == E0M4_OK && weights) rc = launch_kv4_received(a, *s, weights, (hipStream_t)stream);
+    a.scores = p.scores ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes + p.lse_bytes) : nullptr;
+    rc = p.prefill ? launch_kv4_prefill(a, *s, (hipStream_t)stream) : launch_kv4_decode(a, *s, (hipStream_t)stream);
+    if (rc == E0M4_OK && (a.chunks > 1 || p.scores)) rc = launch_kv4_combine(a, *s, p.scores ? weights : nullptr, (hipStream_t)stream);
+    if (rc == E0M4_OK && weights && !p.scores) rc = launch_kv4_received(a, *s, weights, (hipStream_t)stream);
     return rc;
 }
 

@@ -1,16 +1,11 @@
-// Attention of few queries over a cache in E0M4 codes, and the sums of attention that its rows received.  Layout and what it gives
-// the products: e0m4_kv4.h.
+// Attention of few queries over a cache in E0M4 codes, and the sum of its chunks.  Layout and what it gives the products: e0m4_kv4.h;
+// softmax: e0m4_kv4_attention.h.
 //
 // A wavefront takes whole tiles of 32 rows by itself, 16 rows of queries at a time: it reads a tile's codes and parameters with wide
 // loads straight into the operands' lanes, one tile ahead, dequantises them there, and keeps O^T and the softmax's state of its tiles in
 // registers.  Nothing is shared between wavefronts until their results meet at the end: those of a workgroup in LDS, those of a
 // chunk in the workspace, always in the same order.
-//
-// Softmax: p = 2^(t - ref + kShift) with t the score in powers of two.  Any reference gives the same quotient as long as nothing
-// overflows, so it is only moved (and the sums rescaled) when a score exceeds it by more than kSlack: a lane compares its own
-// scores, lanes only meet when one of them does.  P is rounded to fp16 for the product, at most 2^15 and with kShift + 24 = 32 powers
-// of two below the reference; its sum is taken in fp32 before that rounding, whose errors are independent.
-#include "e0m4_kv4.h"
+#include "e0m4_kv4_attention.h"
 #include "e0m4_host.h"
 
 namespace e0m4 {
@@ -18,87 +13,17 @@ namespace e0m4 {
 namespace {
 
 constexpr int kCols = 16;               // rows of queries of a tile
-constexpr float kShift = 8.f, kSlack = 7.f;
-constexpr float kLog2E = 1.44269504088896340736f;
-constexpr float kInf = __builtin_inff();
-
-__device__ inline float bf16_low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-__device__ inline float bf16_high(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
-__device__ inline uint32_t bf16_round(float f)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, f);
-    if (f != f) return 0x7FC0u;
-    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
-
-// Four dims of a row's result from its sums; zeros for a row that sees nothing.
-template <int DIM>
-__device__ inline void finish(const Kv4Attention& a, int b, int h, int row, int d, bool valid, floatx4 acc, float ref, float sum)
-{
-    const float f = !valid || sum == 0.f ? 0.f : 1.f / sum;
-    const int i = row / a.share, head = h * a.share + row % a.share;
-    uint16_t* p = static_cast<uint16_t*>(a.out) + (((int64_t)b * a.n_new + i) * (a.kv_heads * a.share) + head) * DIM + d;
-    uint32_t x[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float y = f == 0.f ? 0.f : acc[j] * f;
-        x[j] = a.bf16 ? bf16_round(y) : (uint32_t)__builtin_bit_cast(uint16_t, (half_t)y);
-    }
-    *reinterpret_cast<uint2*>(p) = uint2{x[0] | (x[1] << 16), x[2] | (x[3] << 16)};
-    if (a.lse && d == 0)
-        a.lse[((int64_t)b * a.kv_heads + h) * ((int64_t)a.n_new * a.share) + row] = f == 0.f ? kInf : ref - kShift + __builtin_amdgcn_logf(sum);
-}
-
-// The lane's part of 16 rows of queries as the right operand of S^T = K Q^T: row row0 + lane % 16, dims kq * DIM/4 + 8 w.  The values
-// of the cache are fp16, so queries are too; bfloat16 ones are scaled by the power of two that brings their row's largest into
-// [1, 2), which `factor` takes back: what is lost of them then is below 2^-25 of the largest.
+// The lane's part of 16 rows of queries as the right operand of S^T = K Q^T: row row0 + lane % 16, dims kq * DIM/4 + 8 w.
 template <int DIM>
 struct Queries {
     half8_t q[DIM / 32];
-    float factor;                       // of a score, to powers of two
+    float factor;
 };
 template <int DIM>
 __device__ inline Queries<DIM> load_queries(const Kv4Attention& a, int b, int h, int row, bool there, int kq)
 {
     Queries<DIM> out;
-    out.factor = kLog2E / __builtin_sqrtf((float)DIM);
-    const int i = row / a.share, head = h * a.share + row % a.share;
-    const uint16_t* p = static_cast<const uint16_t*>(a.q.data) + b * a.q.batch_ld + i * a.q.row_ld + head * a.q.head_ld + kq * (DIM / 4);
-    uint4 raw[DIM / 32];
-#pragma unroll
-    for (int w = 0; w < DIM / 32; ++w) raw[w] = there ? *reinterpret_cast<const uint4*>(p + 8 * w) : uint4{0, 0, 0, 0};
-    if (!a.bf16) {
-#pragma unroll
-        for (int w = 0; w < DIM / 32; ++w) out.q[w] = __builtin_bit_cast(half8_t, raw[w]);
-        return out;
-    }
-    uint32_t top = 0;                   // largest magnitude, as bits
-#pragma unroll
-    for (int w = 0; w < DIM / 32; ++w) {
-        const uint32_t x[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t l = x[j] & 0x7FFFu, u = (x[j] >> 16) & 0x7FFFu;
-            top = l > top ? l : top;
-            top = u > top ? u : top;
-        }
-    }
-    uint32_t o = __shfl_xor(top, 16);
-    top = o > top ? o : top;
-    o = __shfl_xor(top, 32);
-    top = o > top ? o : top;
-    int e = (int)(top >> 7) - 127;
-    if (e == 128 || top == 0) e = 0;    // infinite, not a number, or all zeros
-#pragma unroll
-    for (int w = 0; w < DIM / 32; ++w) {
-        const uint32_t x[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            out.q[w][2 * j] = (half_t)__builtin_ldexpf(bf16_low(x[j]), -e);
-            out.q[w][2 * j + 1] = (half_t)__builtin_ldexpf(bf16_high(x[j]), -e);
-        }
-    }
-    out.factor = __builtin_ldexpf(out.factor, e);
+    out.factor = load_query_row<DIM, DIM / 32, 16>(a, b, h, row, there, kq * (DIM / 4), 8, out.q);
     return out;
 }
 
@@ -108,10 +33,6 @@ struct RawK {
     words4_t code[DIM / 64];
     uint32_t param[2][Kv4<DIM, G>::kLaneGroups];
 };
-__device__ inline words4_t load16(__amdgpu_buffer_rsrc_t tile, int offset)
-{
-    return __builtin_bit_cast(words4_t, __builtin_amdgcn_raw_buffer_load_b128(tile, offset, 0, 0));
-}
 template <int DIM, int G>
 __device__ inline void load_k(__amdgpu_buffer_rsrc_t tile, int lane, RawK<DIM, G>& k)
 {
@@ -169,20 +90,14 @@ __device__ inline void clear_v(RawV<DIM, G>& v, int row0, int kq, int length)
     }
 }
 
-// Which of a tile's rows the lane's query sees: bit 4 s + i for row 16 s + 4 kq + i.  [from, to): by position.
-__device__ inline uint32_t seen_rows(const Kv4Attention& a, int b, int row0, int kq, int query, int from, int to)
+// Which of a tile's rows the lane's query sees: bit 4 s + i for row 16 s + 4 kq + i.
+__device__ inline uint32_t seen_rows(const Kv4Attention& a, int b, int row0, int kq, int query, const Kv4Seen& by_place)
 {
+    auto row_of = [&](int i) { return row0 + 16 * (i >> 2) + 4 * kq + (i & 3); };
     uint32_t seen = 0;
-    const uint8_t* m = a.mask ? a.mask + b * a.mask_batch_ld + query * a.mask_row_ld : nullptr;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 16 * s + 4 * kq + i;
-            bool in = row >= from && row < to;
-            if (m && in) in = row < a.mask_rows && m[row] != 0;
-            seen |= in ? 1u << (4 * s + i) : 0u;
-        }
+    for (int i = 0; i < 8; ++i) seen |= row_of(i) >= by_place.from && row_of(i) < by_place.to ? 1u << i : 0u;
+    if (a.mask) seen &= kv4_mask_bits<2>(a, b, query, [&](int g) { return row_of(4 * g); });
     return seen;
 }
 
@@ -200,13 +115,12 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_decode_kernel(Kv4Attention a)
     const int tile1 = tile0 + a.chunk_tiles < tiles_end ? tile0 + a.chunk_tiles : tiles_end;
     if (tile0 >= tile1 && a.chunks > 1) return;                             // (the sum knows)
 
-    const int query = (row0 + col) / a.share, at = span.length - span.count + query;
+    const int query = kv4_query_of(a, row0 + col), at = span.length - span.count + query;
     const bool valid = col < cols && query < span.count;
     const Queries<DIM> qs = load_queries<DIM>(a, b, h, valid ? row0 + col : 0, valid, kq);
-    const int to = a.causal && at + 1 < span.length ? at + 1 : span.length;
-    const int from = a.window && at - a.window + 1 > 0 ? at - a.window + 1 : 0;
+    const Kv4Seen by_place = kv4_seen(a, span.length, at);
     // rows that all of the tile's queries see by position
-    const int first_query = row0 / a.share, last_query = (row0 + cols - 1) / a.share < span.count ? (row0 + cols - 1) / a.share : span.count - 1;
+    const int first_query = kv4_query_of(a, row0), end_query = kv4_query_of(a, row0 + cols - 1), last_query = end_query < span.count ? end_query : span.count - 1;
     const int all_from = a.window ? span.length - span.count + last_query - a.window + 1 : 0;
     const int all_to = a.causal ? span.length - span.count + first_query + 1 : span.length;
 
@@ -237,12 +151,17 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_decode_kernel(Kv4Attention a)
         load_k(next, lane, k);
         const int r0 = tile * kKv4Rows;
         if (a.mask || r0 < all_from || r0 + kKv4Rows > all_to) {
-            const uint32_t seen = seen_rows(a, b, r0, kq, valid ? query : 0, from, to);
+            const uint32_t seen = seen_rows(a, b, r0, kq, valid ? query : 0, by_place);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[u][i] = (seen >> (4 * u + i)) & 1 ? s[u][i] : -kInf;
             if (r0 + kKv4Rows > span.length) clear_v<DIM, G>(v, r0, kq, span.length);
+        }
+        if (a.scores && valid) {
+            float* out = a.scores + (((int64_t)b * a.kv_heads + h) * rows + row0 + col) * (a.tiles * kKv4Rows) + r0 + 4 * kq;
+            *reinterpret_cast<floatx4*>(out) = s[0] * qs.factor;
+            *reinterpret_cast<floatx4*>(out + 16) = s[1] * qs.factor;
         }
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top *= qs.factor;
@@ -311,145 +230,137 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_decode_kernel(Kv4Attention a)
             *reinterpret_cast<floatx4*>(a.part_out + at_row * DIM + d) = acc;
             if (d == 0) a.part_stats[at_row] = float2{top, total};
         } else {
-            finish<DIM>(a, b, h, row, d, row / a.share < span.count, acc, top, total);
+            finish<DIM>(a, b, h, row, d, kv4_query_of(a, row) < span.count, acc, top, total);
         }
     }
 }
 
-// The sum over chunks, one workgroup per (sequence, head, row), a thread per four dims and quarter of the chunks.
-template <int DIM>
-__global__ __launch_bounds__(DIM) void kv4_combine_kernel(Kv4Attention a)
+// What chunks' results count for in a row's: 2^(reference - largest reference), by the lanes of a wavefront; returns the softmax's sum.
+__device__ inline float chunk_factors(const float2* stats, int64_t stride, int chunks, int lane, float& top, float* factor)
 {
-    constexpr int kParts = 4, kPer = DIM / 4;
-    __shared__ floatx4 part[kParts][kPer];
-    const int t = threadIdx.x, row = blockIdx.x, h = blockIdx.y, b = blockIdx.z, rows = a.n_new * a.share;
-    const int row0 = row / a.tile_rows * a.tile_rows;
-    const Kv4Span span = kv4_span(a, b, row0, rows - row0 < a.tile_rows ? rows - row0 : a.tile_rows);
-    const int tiles = (span.end + kKv4Rows - 1) / kKv4Rows - span.begin / kKv4Rows;
-    const int chunks = (tiles + a.chunk_tiles - 1) / a.chunk_tiles;
-    const int64_t stride = (int64_t)a.batch * a.kv_heads * rows, at = ((int64_t)b * a.kv_heads + h) * rows + row;
-    float top = -kInf, total = 0.f;
-    for (int c = 0; c < chunks; ++c) top = fmaxf(top, a.part_stats[c * stride + at].x);
-    const int d = t % kPer * 4, q = t / kPer;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < chunks; ++c) {
-        const float2 st = a.part_stats[c * stride + at];
+    top = -kInf;
+    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, stats[c * stride].x);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float total = 0.f;
+    for (int c = lane; c < chunks; c += 64) {
+        const float2 st = stats[c * stride];
         const float f = top == -kInf ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
+        if (factor) factor[c] = f;
         total += st.y * f;
-        if (c % kParts == q) acc += *reinterpret_cast<const floatx4*>(a.part_out + (c * stride + at) * DIM + d) * f;
     }
-    part[q][t % kPer] = acc;
-    __syncthreads();
-    if (q) return;
 #pragma unroll
-    for (int i = 1; i < kParts; ++i) acc += part[i][t];
-    finish<DIM>(a, b, h, row, d, row / a.share < span.count, acc, top, total);
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    return total;
+}
+__device__ inline int chunks_of(const Kv4Attention& a, int b, int row, int rows, Kv4Span& span)
+{
+    const int row0 = row / a.tile_rows * a.tile_rows;
+    span = kv4_span(a, b, row0, rows - row0 < a.tile_rows ? rows - row0 : a.tile_rows);
+    const int tiles = (span.end + a.tile_keys - 1) / a.tile_keys - span.begin / a.tile_keys;
+    return (tiles + a.chunk_tiles - 1) / a.chunk_tiles;
 }
 
-// What the rows of a tile of the cache received: one workgroup per tile, its wavefronts share the rows of queries.  K stays in
-// registers as operands.
-template <int DIM, int G>
-__global__ __launch_bounds__(256) void kv4_received_kernel(Kv4Attention a, float* __restrict__ received)
+// The sum over chunks, one workgroup per (sequence, head, row): a wavefront works out what they count for, then a thread has four dims
+// of every kParts-th chunk.  Workgroups beyond the rows' add what 256 rows of the cache received, from the scores (tiles of 16 rows
+// of queries, one of them at most).
+constexpr int kCombineThreads = 256, kReceivedRows = 16;
+template <int DIM>
+__global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attention a, float* __restrict__ received)
 {
-    using L = Kv4<DIM, G>;
-    constexpr int kSteps = DIM / 32, kWaves = 4;
-    __shared__ float part[kWaves][kKv4Rows];
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, kq = lane >> 4;
-    const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z, r0 = tile * kKv4Rows, rows = a.n_new * a.share;
-    const int length = clamp_count(a.lengths[b], a.capacity), count = a.counts ? clamp_count(a.counts[b], a.n_new) : a.n_new;
-    if (r0 >= length || count == 0) return;
-    const int64_t bh = (int64_t)b * a.kv_heads + h;
-    // queries that may see one of the tile's rows
-    int i0 = 0, i1 = count;
-    if (a.causal) {
-        const int at = length - count, last = r0 + kKv4Rows < length ? r0 + kKv4Rows - 1 : length - 1;
-        i0 = r0 - at > 0 ? r0 - at : 0;
-        if (a.window && last + a.window - at < i1) i1 = last + a.window - at;
-    }
-    RawK<DIM, G> raw;
-    load_k(make_rsrc(a.cache + (bh * a.tiles + tile) * L::kBytes), lane, raw);
-    const uint32_t hi = frac_mask_vgpr(), lo = frac_mask_low_vgpr();
-    half8_t k[2][kSteps];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int w = 0; w < kSteps; ++w) k[u][w] = operand_k<DIM, G>(raw, u, w, hi, lo);
-    float got[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    for (int row0 = (i0 * a.share) / kCols * kCols + wave * kCols; row0 < i1 * a.share; row0 += kWaves * kCols) {
-        const int row = row0 + col, query = row / a.share, at = length - count + query;
-        const bool valid = row < rows && query < count;
-        const Queries<DIM> qs = load_queries<DIM>(a, b, h, valid ? row : 0, valid, kq);
-        const float lse = valid ? a.lse[bh * rows + row] : kInf;
-        floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-        for (int w = 0; w < kSteps; ++w)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[u][w], qs.q[w], s[u], 0, 0, 0);
-        const int to = a.causal && at + 1 < length ? at + 1 : length;
-        const int from = a.window && at - a.window + 1 > 0 ? at - a.window + 1 : 0;
-        const uint32_t seen = valid ? seen_rows(a, b, r0, kq, query, from, to) : 0u;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((seen >> (4 * u + i)) & 1) got[u][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], qs.factor, -lse));
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float g = got[u][i];
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) g += __shfl_xor(g, d);
-            if (col == 0) part[wave][16 * u + 4 * kq + i] = g;
+    constexpr int kPer = DIM / 4, kParts = kCombineThreads / kPer;
+    __shared__ float factor[kKv4MaxChunks];
+    __shared__ floatx4 part[kParts][kPer];
+    __shared__ float shared[kReceivedRows];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = blockIdx.y, b = blockIdx.z, rows = a.n_new * a.share;
+    const int64_t stride = (int64_t)a.batch * a.kv_heads * rows, bh = (int64_t)b * a.kv_heads + h;
+    const int sums = a.chunks > 1 ? rows : 0;
+    Kv4Span span;
+    if ((int)blockIdx.x < sums) {
+        const int row = blockIdx.x, chunks = chunks_of(a, b, row, rows, span);
+        const int64_t at = bh * rows + row;
+        float top, total;
+        if (wave == 0) {
+            total = chunk_factors(a.part_stats + at, stride, chunks, lane, top, factor);
+            if (lane == 0) {
+                shared[0] = top;
+                shared[1] = total;
+            }
         }
-    __syncthreads();
-    if (t < kKv4Rows && r0 + t < length) {
-        float g = 0.f;
+        __syncthreads();
+        top = shared[0];
+        total = shared[1];
+        const int d = t % kPer * 4, q = t / kPer;
+        const float* p = a.part_out + at * DIM + d;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int c = q; c < chunks; c += kParts) acc += *reinterpret_cast<const floatx4*>(p + c * stride * DIM) * factor[c];
+        part[q][t % kPer] = acc;
+        __syncthreads();
+        if (q) return;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) g += part[w][t];
-        received[bh * a.capacity + r0 + t] += g;
+        for (int i = 1; i < kParts; ++i) acc += part[i][t];
+        finish<DIM>(a, b, h, row, d, kv4_query_of(a, row) < span.count, acc, top, total);
+        return;
     }
+    const int chunks = chunks_of(a, b, 0, rows, span), key = ((int)blockIdx.x - sums) * kCombineThreads + t;
+    if (key - t >= span.end || key - t + kCombineThreads <= span.begin) return;
+    if (a.chunks > 1) {
+        for (int row = wave; row < rows; row += kCombineThreads / 64) {
+            float top;
+            const float total = chunk_factors(a.part_stats + bh * rows + row, stride, chunks, lane, top, nullptr);
+            if (lane == 0) shared[row] = kv4_query_of(a, row) < span.count && total != 0.f ? top - kShift + __builtin_amdgcn_logf(total) : kInf;
+        }
+    } else if (t < rows) {
+        shared[t] = a.lse[bh * rows + t];
+    }
+    __syncthreads();
+    if (key < span.begin / kKv4Rows * kKv4Rows || key >= span.end) return;
+    const float* s = a.scores + bh * rows * (a.tiles * kKv4Rows) + key;
+    float got = 0.f;
+    for (int row = 0; row < rows; ++row) {
+        if (kv4_query_of(a, row) >= span.count) break;  // (their scores were not written)
+        const float x = s[row * (a.tiles * kKv4Rows)];
+        got += x == -kInf ? 0.f : __builtin_amdgcn_exp2f(x - shared[row]);
+    }
+    received[bh * a.capacity + key] += got;
+}
+
+template <int DIM, int G, int WAVES>
+int launch_decode(const Kv4Attention& a, dim3 grid, int cols, hipStream_t stream)
+{
+    const int lds = (WAVES * cols * (DIM + 4) + 2 * WAVES * kCols) * 4;
+    static std::atomic<uint64_t> allowed{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&kv4_decode_kernel<DIM, G, WAVES>), 160 * 1024, allowed);
+    if (rc != E0M4_OK) return rc;
+    hipLaunchKernelGGL((kv4_decode_kernel<DIM, G, WAVES>), grid, dim3(WAVES * 64), lds, stream, a);
+    return check_launch();
 }
 
 }  // namespace
 
 int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream)
 {
-    constexpr int kWaves = 4;
     const int64_t rows = (int64_t)a.n_new * a.share, row_tiles = (rows + kCols - 1) / kCols;
     const int cols = rows < kCols ? (int)rows : kCols;
-    const int lds = (kWaves * cols * (s.dim + 4) + 2 * kWaves * kCols) * 4;
     const dim3 grid((unsigned)(row_tiles * a.chunks), (unsigned)a.kv_heads, (unsigned)a.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        static std::atomic<uint64_t> allowed{0};
-        const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&kv4_decode_kernel<DIM, G, kWaves>), 160 * 1024, allowed);
-        if (rc != E0M4_OK) return rc;
-        hipLaunchKernelGGL((kv4_decode_kernel<DIM, G, kWaves>), grid, dim3(kWaves * 64), lds, stream, a);
-        return check_launch();
+        if (a.chunks > 1 || a.chunk_tiles > kKv4ShortTiles) return launch_decode<DIM, G, 4>(a, grid, cols, stream);
+        return launch_decode<DIM, G, DIM == 256 ? 8 : 16>(a, grid, cols, stream);
     });
 }
 
-int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream)
+int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.n_new * a.share), (unsigned)a.kv_heads, (unsigned)a.batch);
+    const int64_t blocks = received ? (s.capacity + kCombineThreads - 1) / kCombineThreads : 0;
+    const dim3 grid((unsigned)((a.chunks > 1 ? a.n_new * a.share : 0) + blocks), (unsigned)a.kv_heads, (unsigned)a.batch);
     switch (s.dim) {
-        case 64: hipLaunchKernelGGL(kv4_combine_kernel<64>, grid, dim3(64), 0, stream, a); break;
-        case 128: hipLaunchKernelGGL(kv4_combine_kernel<128>, grid, dim3(128), 0, stream, a); break;
-        default: hipLaunchKernelGGL(kv4_combine_kernel<256>, grid, dim3(256), 0, stream, a); break;
+        case 64: hipLaunchKernelGGL(kv4_combine_kernel<64>, grid, dim3(kCombineThreads), 0, stream, a, received); break;
+        case 128: hipLaunchKernelGGL(kv4_combine_kernel<128>, grid, dim3(kCombineThreads), 0, stream, a, received); break;
+        default: hipLaunchKernelGGL(kv4_combine_kernel<256>, grid, dim3(kCombineThreads), 0, stream, a, received); break;
     }
     return check_launch();
-}
-
-int launch_kv4_received(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream)
-{
-    const dim3 grid((unsigned)a.tiles, (unsigned)a.kv_heads, (unsigned)a.batch);
-    return kv4_dispatch(s, [&](auto shape) -> int {
-        constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        hipLaunchKernelGGL((kv4_received_kernel<DIM, G>), grid, dim3(256), 0, stream, a, received);
-        return check_launch();
-    });
 }
 
 }  // namespace e0m4

@@ -24,6 +24,14 @@ def e0m4():
     return pkg
 
 
+@pytest.fixture(params=["chosen", "few", "many", "wide"])
+def kernels(request, e0m4):
+    """The kernel that the library chooses, and each of them on everything."""
+    e0m4.e0m4_set_knob("kv4_attention", {"chosen": 0, "few": 1, "many": 2, "wide": 3}[request.param])
+    yield request.param
+    e0m4.e0m4_set_knob("kv4_attention", 0)
+
+
 def dirty(e0m4, shape):
     return e0m4.e0m4_kv4_alloc(shape, DEV).fill_(255)
 
@@ -211,7 +219,7 @@ def check_attention(e0m4, oracle, dim, group, kv, share, n, lengths, counts=None
 
 @pytest.mark.parametrize("dim,group", SHAPES)
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
-def test_single_tokens(e0m4, oracle, dim, group, dtype):
+def test_single_tokens(e0m4, oracle, kernels, dim, group, dtype):
     check_attention(e0m4, oracle, dim, group, 2, 1, 1, [1, 31, 32, 33, 300], dtype=dtype, weights=True)
     check_attention(e0m4, oracle, dim, group, 1, 16, 1, [700, 5], dtype=dtype)
     check_attention(e0m4, oracle, dim, group, 2, 3, 1, [0, 65, 2000], dtype=dtype, capacity=2050, weights=True)
@@ -219,34 +227,34 @@ def test_single_tokens(e0m4, oracle, dim, group, dtype):
 
 @pytest.mark.parametrize("dim,group", SHAPES)
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
-def test_prompts(e0m4, oracle, dim, group, dtype):
+def test_prompts(e0m4, oracle, kernels, dim, group, dtype):
     check_attention(e0m4, oracle, dim, group, 2, 2, 130, [130, 101], counts=[130, 101], dtype=dtype, weights=True)
     check_attention(e0m4, oracle, dim, group, 1, 5, 77, [400, 77, 90], counts=[77, 70, 1], dtype=dtype, weights=True)
     check_attention(e0m4, oracle, dim, group, 1, 1, 300, [300], dtype=dtype)
 
 
 @pytest.mark.parametrize("n", [2, 3, 8, 15, 16, 17, 31, 33, 48, 63, 64, 65, 100, 128, 129, 200])
-def test_numbers_of_new_tokens(e0m4, oracle, n):
+def test_numbers_of_new_tokens(e0m4, oracle, kernels, n):
     check_attention(e0m4, oracle, 128, 128, 1, 1, n, [n + 5, n, 333], weights=True, seed=n)
     check_attention(e0m4, oracle, 128, 64, 2, 7, n, [n + 64], dtype=torch.bfloat16, seed=n)
 
 
 @pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 100, 1000])
 @pytest.mark.parametrize("n,share", [(1, 4), (9, 4), (150, 2)])
-def test_windows(e0m4, oracle, window, n, share):
+def test_windows(e0m4, oracle, kernels, window, n, share):
     check_attention(e0m4, oracle, 64, 32, 2, share, n, [700, 150, 333], window=window, weights=True, seed=window, counts=[n, n, min(n, 5)])
     check_attention(e0m4, oracle, 128, 128, 1, share, n, [290], window=window, seed=window)
 
 
 @pytest.mark.parametrize("n,share", [(1, 1), (4, 8), (40, 2), (140, 1)])
-def test_every_query_sees_every_row(e0m4, oracle, n, share):
+def test_every_query_sees_every_row(e0m4, oracle, kernels, n, share):
     check_attention(e0m4, oracle, 128, 64, 2, share, n, [140, 200, 0], counts=[n, max(n - 3, 0), 0], causal=False, weights=True)
     check_attention(e0m4, oracle, 256, 128, 1, share, n, [63], causal=False)
 
 
 @pytest.mark.parametrize("n,share", [(1, 2), (12, 16), (50, 3), (129, 2)])
 @pytest.mark.parametrize("causal", [True, False])
-def test_masks(e0m4, oracle, n, share, causal):
+def test_masks(e0m4, oracle, kernels, n, share, causal):
     gen = torch.Generator().manual_seed(n)
     mask = torch.rand((2, n, 300), generator=gen) < 0.3
     mask[0, n // 2] = False                                          # a row with nothing
@@ -260,20 +268,20 @@ def test_masks(e0m4, oracle, n, share, causal):
     check_attention(e0m4, oracle, 128, 64, 1, share, n, [300, 211], mask=torch.zeros((1, 1, 300), dtype=torch.bool), causal=causal)
 
 
-def test_masks_and_windows_together(e0m4, oracle):
+def test_masks_and_windows_together(e0m4, oracle, kernels):
     gen = torch.Generator().manual_seed(3)
     mask = torch.rand((1, 20, 500), generator=gen) < 0.5
     check_attention(e0m4, oracle, 128, 128, 2, 4, 20, [500, 60], mask=mask, window=37, weights=True)
 
 
 @pytest.mark.parametrize("strong", [0.0, 1e-3, 30.0])
-def test_flat_and_sharp_scores(e0m4, oracle, strong):
+def test_flat_and_sharp_scores(e0m4, oracle, kernels, strong):
     for n in (1, 90):
         check_attention(e0m4, oracle, 128, 128, 1, 4, n, [1500, 700], strong=strong, weights=True)
         check_attention(e0m4, oracle, 64, 64, 2, 1, n, [1500], strong=strong, dtype=torch.bfloat16)
 
 
-def test_scores_that_rise_along_the_cache(e0m4, oracle):
+def test_scores_that_rise_along_the_cache(e0m4, oracle, kernels):
     """The reference of the softmax has to move many times, also far after the first rows."""
     dim, rows = 128, 3000
     shape = e0m4.E0M4KV4Shape(1, 1, rows, dim, 128)
@@ -293,7 +301,7 @@ def test_scores_that_rise_along_the_cache(e0m4, oracle):
         assert ((got.cpu().double() - received).abs() <= plain.received_bounds(received, reach, dim, 2 * n)).all()
 
 
-def test_queries_out_of_the_ordinary(e0m4, oracle):
+def test_queries_out_of_the_ordinary(e0m4, oracle, kernels):
     """bfloat16 queries far outside fp16's range; queries that are not finite touch their own row only."""
     dim, rows, kv = 128, 200, 1
     gen = torch.Generator().manual_seed(4)
@@ -324,7 +332,7 @@ def test_queries_out_of_the_ordinary(e0m4, oracle):
         assert same_bits(out2[:, rest], out[:, rest])
 
 
-def test_lengths_and_counts_out_of_range_are_taken_as_the_nearest(e0m4, oracle):
+def test_lengths_and_counts_out_of_range_are_taken_as_the_nearest(e0m4, oracle, kernels):
     gen = torch.Generator().manual_seed(8)
     shape = e0m4.E0M4KV4Shape(4, 1, 70, 64, 64)
     cache = dirty(e0m4, shape)
@@ -340,13 +348,13 @@ def test_lengths_and_counts_out_of_range_are_taken_as_the_nearest(e0m4, oracle):
     assert (a[2, :2] == 0).all() and (a[2, 2:] != 0).any()           # the first of five queries over three rows stand before the first row
 
 
-def test_long_caches(e0m4, oracle):
+def test_long_caches(e0m4, oracle, kernels):
     check_attention(e0m4, oracle, 64, 64, 1, 4, 1, [40000, 7], weights=True)
     check_attention(e0m4, oracle, 128, 128, 1, 8, 3, [20000], dtype=torch.bfloat16)
     check_attention(e0m4, oracle, 64, 32, 1, 1, 70, [9000], weights=True)
 
 
-def test_offsets_beyond_32_bits(e0m4, oracle):
+def test_offsets_beyond_32_bits(e0m4, oracle, kernels):
     """A cache of more than 4 GiB, rows at its end."""
     gen = torch.Generator().manual_seed(9)
     dim, group, capacity = 256, 32, 14_000_000
@@ -367,7 +375,7 @@ def test_offsets_beyond_32_bits(e0m4, oracle):
         assert ((out.cpu().double() - want).abs() <= plain.attention_bounds(want, size, reach, dim, n, torch.float16)).all()
 
 
-def test_attention_of_nothing(e0m4):
+def test_attention_of_nothing(e0m4, kernels):
     shape = e0m4.E0M4KV4Shape(2, 2, 0, 64, 64)
     cache = e0m4.e0m4_kv4_alloc(shape, DEV)
     out = torch.full((2, 3, 4, 64), 7.0, dtype=torch.float16, device=DEV)
