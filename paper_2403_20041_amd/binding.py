@@ -9,6 +9,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple
 
@@ -368,39 +369,49 @@ def e0m4_kv_append(cache, new_rows, position_ids, stream=None):
 _KV4_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 
+@functools.lru_cache(maxsize=256)
+def _kv4_shape(shape):
+    """(the C struct, bytes of a cache) of a shape: both are its alone, and a call asks for them each time."""
+    c = _KV4Shape(*shape)
+    return c, lib().e0m4_kv4_bytes(c)
+
+
 def _kv4_per_sequence(t, shape, name: str, where: str):
     """Device int32 [batch], or None."""
-    if t is not None and (t.dtype != torch.int32 or t.shape != (shape.batch,) or not t.is_contiguous() or not t.is_cuda):
+    if t is None:
+        return 0
+    if t.dtype is not torch.int32 or t.shape != (shape[0],) or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("%s: %s must be a contiguous cuda int32 tensor of shape (%d,), got %s %s on %s"
-                         % (where, name, shape.batch, t.dtype, tuple(t.shape), t.device))
-    return _ptr(t)
+                         % (where, name, shape[0], t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
 
 
 def _kv4_rows(t, n: int, heads: int, shape, name: str, where: str):
     """A [batch, n, heads, dim] tensor of any strides but the last."""
     if t.dtype not in _KV4_DTYPES:
         raise TypeError("%s: %s must be float16 or bfloat16" % (where, name))
-    if t.shape != (shape.batch, n, heads, shape.dim) or (t.numel() and t.stride(3) != 1) or not t.is_cuda:
+    batch, dim = shape[0], shape[3]
+    ld = t.stride()
+    if t.shape != (batch, n, heads, dim) or not t.is_cuda or (ld[3] != 1 and t.numel()):
         raise ValueError("%s: %s must be a cuda tensor of shape %s whose last dimension is contiguous, got %s with strides %s on %s"
-                         % (where, name, (shape.batch, n, heads, shape.dim), tuple(t.shape), t.stride(), t.device))
+                         % (where, name, (batch, n, heads, dim), tuple(t.shape), ld, t.device))
     # (the stride of a dimension of one is never walked, whatever it says)
-    ld = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
-    return _KV4Rows(t.data_ptr(), *ld)
+    return _KV4Rows(t.data_ptr(), ld[0] if batch > 1 else 0, ld[1] if n > 1 else 0, ld[2] if heads > 1 else 0)
 
 
 def _kv4_cache(cache, shape, name: str, where: str):
-    need = e0m4_kv4_bytes(shape)
-    if cache.dtype != torch.uint8 or not cache.is_contiguous() or not cache.is_cuda or cache.numel() < need:
+    c, need = _kv4_shape(shape)
+    if cache.dtype is not torch.uint8 or not cache.is_contiguous() or not cache.is_cuda or cache.numel() < need:
         raise ValueError("%s: %s must be a contiguous cuda uint8 tensor of at least %d bytes" % (where, name, need))
-    return _KV4Shape(*shape)
+    return c
 
 
 def e0m4_kv4_bytes(shape: E0M4KV4Shape) -> int:
-    return lib().e0m4_kv4_bytes(_KV4Shape(*shape))
+    return _kv4_shape(shape)[1]
 
 
 def e0m4_kv4_attention_workspace_bytes(shape: E0M4KV4Shape, heads: int, n_new: int, with_weights: bool = False) -> int:
-    return lib().e0m4_kv4_attention_workspace_bytes(_KV4Shape(*shape), heads, n_new, 1 if with_weights else 0)
+    return lib().e0m4_kv4_attention_workspace_bytes(_kv4_shape(shape)[0], heads, n_new, 1 if with_weights else 0)
 
 
 def e0m4_kv4_alloc(shape: E0M4KV4Shape, device) -> torch.Tensor:
@@ -416,7 +427,8 @@ def e0m4_kv4_append(cache, shape: E0M4KV4Shape, keys, values, starts, counts=Non
     cache from row starts[b] on, the first counts[b] of them (None: all)."""
     where = "e0m4_kv4_append"
     n = keys.shape[1]
-    k, v = (_kv4_rows(t, n, shape.kv_heads, shape, name, where) for t, name in ((keys, "keys"), (values, "values")))
+    k = _kv4_rows(keys, n, shape[1], shape, "keys", where)
+    v = _kv4_rows(values, n, shape[1], shape, "values", where)
     if keys.dtype != values.dtype:
         raise TypeError("e0m4_kv4_append: keys and values must be of one type")
     _check(lib().e0m4_kv4_append(_ptr(cache), _kv4_cache(cache, shape, "cache", where), k, v, _KV4_DTYPES[keys.dtype], n,
@@ -430,7 +442,9 @@ def e0m4_kv4_read(cache, shape: E0M4KV4Shape, lengths, rows: int, first=None, st
     where = "e0m4_kv4_read"
     s = _kv4_cache(cache, shape, "cache", where)
     size = (shape.batch, max(rows, 0), shape.kv_heads, shape.dim)
-    keys, values = (_empty(size, torch.float16, cache.device, stream, "cache's rows") for _ in range(2))
+    device = cache.device
+    keys = _empty(size, torch.float16, device, stream, "keys")
+    values = _empty(size, torch.float16, device, stream, "values")
     _check(lib().e0m4_kv4_read(_ptr(cache), s, _kv4_per_sequence(lengths, shape, "lengths", where),
                                _kv4_per_sequence(first, shape, "first", where), rows, _ptr(keys), _ptr(values), _stream(stream)), where)
     return keys, values

@@ -30,6 +30,7 @@ const char* const kKnobNames[] = {      // in the order of Knob
     "gemm_panel",                 // row tiles per panel of the pipelined GEMM's tile numbering (0: the default, -1: whole columns)
     "gemm_split_order",           // work items of a K-split launch: 1 by tile, 2 by split (0: by the length of a split)
     "kv4_attention",              // attention over a cache in 4 bits: 1 the kernel for few queries, 2 the one for many, 3 that with 256 rows to a workgroup
+    "kv4_chunk",                  // ... tiles of the cache to a workgroup
 };
 static_assert(sizeof(kKnobNames) / sizeof(kKnobNames[0]) == (size_t)Knob::count, "a name for each");
 

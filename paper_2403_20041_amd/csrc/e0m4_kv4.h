@@ -142,6 +142,8 @@ struct Kv4Attention {
     float* part_out;                                    // [chunk][batch][kv_heads][rows][dim]
     float2* part_stats;                                 // [chunk][batch][kv_heads][rows]: reference exponent, sum
     float* lse;                                         // [batch][kv_heads][rows] log2 of the softmax's sum, for the received weights
+    half_t* packed_q;                                   // [batch][kv_heads][rows][dim] queries as the products take them, and
+    float* factors;                                     // [batch][kv_heads][rows] their scores' factors, or null
     float* scores;                                      // [batch][kv_heads][rows][tiles * 32] in powers of two, or null
 };
 

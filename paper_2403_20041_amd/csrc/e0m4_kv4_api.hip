@@ -40,8 +40,8 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 struct Plan {
     bool prefill, scores;
     int tile_rows, tile_keys, chunk_tiles, chunks;
-    size_t out_bytes, stats_bytes, lse_bytes, scores_bytes;
-    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes + scores_bytes; }
+    size_t out_bytes, stats_bytes, lse_bytes, scores_bytes, queries_bytes;
+    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes + scores_bytes + queries_bytes; }
 };
 Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool weights)
 {
@@ -59,10 +59,12 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
         chunk = n > 128 ? tiles : (tiles + 256 / n - 1) / (256 / n);
     } else {
         p.tile_rows = 16;
-        chunk = tiles * sets(16) / 2048;
+        chunk = tiles * sets(16) / 3072;
+        if (chunk < 8) chunk = 8;
         if (tiles <= kKv4ShortTiles) chunk = tiles;
     }
     if (chunk < 4) chunk = 4;
+    if (knob(Knob::kv4_chunk) > 0) chunk = knob(Knob::kv4_chunk);
     if (chunk < (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks) chunk = (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks;
     if (chunk > tiles) chunk = tiles;
     p.chunk_tiles = (int)chunk;
@@ -71,6 +73,7 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     p.out_bytes = p.chunks > 1 ? (size_t)p.chunks * all * s.dim * 4 : 0;
     p.stats_bytes = p.chunks > 1 ? round16((size_t)p.chunks * all * 8) : 0;
     p.lse_bytes = weights ? round16((size_t)all * 4) : 0;
+    p.queries_bytes = weights && !p.scores ? (size_t)all * s.dim * 2 + round16((size_t)all * 4) : 0;
     p.scores_bytes = p.scores ? (size_t)all * kv4_tiles(s.capacity) * kKv4Rows * 4 : 0;
     return p;
 }
@@ -196,6 +199,10 @@ int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, i
     a.part_out = reinterpret_cast<float*>(w);
     a.part_stats = reinterpret_cast<float2*>(w + p.out_bytes);
     a.lse = weights ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes) : nullptr;
+    if (p.queries_bytes) {
+        a.packed_q = reinterpret_cast<half_t*>(w + p.out_bytes + p.stats_bytes + p.lse_bytes);
+        a.factors = reinterpret_cast<float*>(a.packed_q + (size_t)a.batch * heads * n_new * s->dim);
+    }
     a.scores = p.scores ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes + p.lse_bytes) : nullptr;
     rc = p.prefill ? launch_kv4_prefill(a, *s, (hipStream_t)stream) : launch_kv4_decode(a, *s, (hipStream_t)stream);
     if (rc == E0M4_OK && (a.chunks > 1 || p.scores)) rc = launch_kv4_combine(a, *s, p.scores ? weights : nullptr, (hipStream_t)stream);

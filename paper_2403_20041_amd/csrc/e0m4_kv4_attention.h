@@ -106,6 +106,16 @@ __device__ inline float load_query_row(const Kv4Attention& a, int b, int h, int 
     return __builtin_ldexpf(factor, e);
 }
 
+// The same row for the pass over the received weights; zeros where there is no query.
+template <int N>
+__device__ inline void keep_query_row(const Kv4Attention& a, int64_t row, int dim, bool there, int first, int step, const half8_t (&q)[N], float factor)
+{
+#pragma unroll
+    for (int w = 0; w < N; ++w)
+        *reinterpret_cast<half8_t*>(a.packed_q + row * dim + first + step * w) = there ? q[w] : half8_t{0, 0, 0, 0, 0, 0, 0, 0};
+    if (first < 8) a.factors[row] = there ? factor : 0.f;
+}
+
 // Rows of the cache that a query at position `at` sees, by position: [from, to).
 struct Kv4Seen {
     int from, to;

@@ -102,43 +102,54 @@ __device__ inline uint32_t seen_rows(const Kv4Attention& a, int b, int row0, int
 }
 
 template <int DIM, int G, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void kv4_decode_kernel(Kv4Attention a)
+__global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 ? 3 : 4) void kv4_decode_kernel(Kv4Attention a)
 {
     using L = Kv4<DIM, G>;
     constexpr int kSteps = DIM / 32, kDimTiles = DIM / 16, kStride = DIM + 4;
     extern __shared__ __attribute__((aligned(16))) float shared[];          // [wave][column][DIM + 4], then the statistics
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, kq = lane >> 4;
-    const int b = blockIdx.z, h = blockIdx.y, chunk = blockIdx.x % a.chunks, row0 = blockIdx.x / a.chunks * kCols;
+    // (chunks are rotated from head to head: with a multiple of eight of them each would be one XCD's everywhere, and the last ones,
+    // which short sequences do not have, leave theirs idle)
+    const int b = blockIdx.z, h = blockIdx.y, chunk = (blockIdx.x + blockIdx.y + blockIdx.z * gridDim.y) % a.chunks, row0 = blockIdx.x / a.chunks * kCols;
     const int rows = a.n_new * a.share, cols = rows - row0 < kCols ? rows - row0 : kCols;
+    const uint8_t* cache = a.cache + ((int64_t)b * a.kv_heads + h) * a.tiles * L::kBytes;
+    RawK<DIM, G> k;
+    RawV<DIM, G> v;
+    // where a workgroup has all of a sequence's rows, its first tiles are on their way before their number is known
+    const bool early = WAVES > 4 && a.window == 0;
+    if (early) {
+        const __amdgpu_buffer_rsrc_t first = rsrc_if(cache + (int64_t)wave * L::kBytes, wave < a.tiles);
+        load_k(first, lane, k);
+        load_v(first, lane, v);
+    }
     const Kv4Span span = kv4_span(a, b, row0, cols);
     const int tile0 = span.begin / kKv4Rows + chunk * a.chunk_tiles, tiles_end = (span.end + kKv4Rows - 1) / kKv4Rows;
     const int tile1 = tile0 + a.chunk_tiles < tiles_end ? tile0 + a.chunk_tiles : tiles_end;
-    if (tile0 >= tile1 && a.chunks > 1) return;                             // (the sum knows)
-
     const int query = kv4_query_of(a, row0 + col), at = span.length - span.count + query;
     const bool valid = col < cols && query < span.count;
-    const Queries<DIM> qs = load_queries<DIM>(a, b, h, valid ? row0 + col : 0, valid, kq);
+    // (rows from the sequence's count on are read too, so that nobody waits for it; their results are not used)
+    const Queries<DIM> qs = load_queries<DIM>(a, b, h, col < cols ? row0 + col : 0, col < cols, kq);
+    if (a.packed_q && chunk == 0 && col < cols)
+        keep_query_row<kSteps>(a, ((int64_t)b * a.kv_heads + h) * rows + row0 + col, DIM, valid, kq * (DIM / 4), 8, qs.q, qs.factor);
+    if (tile0 >= tile1 && a.chunks > 1) return;                             // (the sum knows)
     const Kv4Seen by_place = kv4_seen(a, span.length, at);
     // rows that all of the tile's queries see by position
     const int first_query = kv4_query_of(a, row0), end_query = kv4_query_of(a, row0 + cols - 1), last_query = end_query < span.count ? end_query : span.count - 1;
     const int all_from = a.window ? span.length - span.count + last_query - a.window + 1 : 0;
     const int all_to = a.causal ? span.length - span.count + first_query + 1 : span.length;
 
-    const uint8_t* cache = a.cache + ((int64_t)b * a.kv_heads + h) * a.tiles * L::kBytes;
+    int tile = tile0 + wave;
+    if (!early) {
+        const __amdgpu_buffer_rsrc_t first = rsrc_if(cache + (int64_t)tile * L::kBytes, tile < tile1);
+        load_k(first, lane, k);
+        load_v(first, lane, v);
+    }
     const uint32_t hi = frac_mask_vgpr(), lo = frac_mask_low_vgpr();
     floatx4 o[kDimTiles];
 #pragma unroll
     for (int d = 0; d < kDimTiles; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
     float ref = -kInf, sum = 0.f;
 
-    RawK<DIM, G> k;
-    RawV<DIM, G> v;
-    int tile = tile0 + wave;
-    {
-        const __amdgpu_buffer_rsrc_t first = rsrc_if(cache + (int64_t)tile * L::kBytes, tile < tile1);
-        load_k(first, lane, k);
-        load_v(first, lane, v);
-    }
     for (; tile < tile1; tile += WAVES) {
         // (behind the last one there is no access to memory)
         const __amdgpu_buffer_rsrc_t next = rsrc_if(cache + (int64_t)(tile + WAVES) * L::kBytes, tile + WAVES < tile1);
@@ -262,9 +273,9 @@ __device__ inline int chunks_of(const Kv4Attention& a, int b, int row, int rows,
 }
 
 // The sum over chunks, one workgroup per (sequence, head, row): a wavefront works out what they count for, then a thread has four dims
-// of every kParts-th chunk.  Workgroups beyond the rows' add what 256 rows of the cache received, from the scores (tiles of 16 rows
+// of every kParts-th chunk.  Workgroups beyond the rows' add what 2048 rows of the cache received, from the scores (tiles of 16 rows
 // of queries, one of them at most).
-constexpr int kCombineThreads = 256, kReceivedRows = 16;
+constexpr int kCombineThreads = 256, kReceivedRows = 16, kReceivedKeys = 2048;
 template <int DIM>
 __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attention a, float* __restrict__ received)
 {
@@ -303,8 +314,8 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
         finish<DIM>(a, b, h, row, d, kv4_query_of(a, row) < span.count, acc, top, total);
         return;
     }
-    const int chunks = chunks_of(a, b, 0, rows, span), key = ((int)blockIdx.x - sums) * kCombineThreads + t;
-    if (key - t >= span.end || key - t + kCombineThreads <= span.begin) return;
+    const int chunks = chunks_of(a, b, 0, rows, span), key0 = ((int)blockIdx.x - sums) * kReceivedKeys;
+    if (key0 >= span.end || key0 + kReceivedKeys <= span.begin) return;
     if (a.chunks > 1) {
         for (int row = wave; row < rows; row += kCombineThreads / 64) {
             float top;
@@ -315,15 +326,29 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
         shared[t] = a.lse[bh * rows + t];
     }
     __syncthreads();
-    if (key < span.begin / kKv4Rows * kKv4Rows || key >= span.end) return;
-    const float* s = a.scores + bh * rows * (a.tiles * kKv4Rows) + key;
-    float got = 0.f;
+    const int low = span.begin / kKv4Rows * kKv4Rows;
+    const float* s = a.scores + bh * rows * (a.tiles * kKv4Rows);
+    float* out = received + bh * a.capacity;
+    int key[kReceivedKeys / kCombineThreads];
+    float got[kReceivedKeys / kCombineThreads], old[kReceivedKeys / kCombineThreads];
+#pragma unroll
+    for (int j = 0; j < kReceivedKeys / kCombineThreads; ++j) {
+        key[j] = key0 + t + j * kCombineThreads;
+        key[j] = key[j] >= low && key[j] < span.end ? key[j] : -1;
+        got[j] = 0.f;
+        old[j] = key[j] >= 0 ? out[key[j]] : 0.f;
+    }
     for (int row = 0; row < rows; ++row) {
         if (kv4_query_of(a, row) >= span.count) break;  // (their scores were not written)
-        const float x = s[row * (a.tiles * kKv4Rows)];
-        got += x == -kInf ? 0.f : __builtin_amdgcn_exp2f(x - shared[row]);
+#pragma unroll
+        for (int j = 0; j < kReceivedKeys / kCombineThreads; ++j) {
+            const float x = key[j] >= 0 ? s[row * (a.tiles * kKv4Rows) + key[j]] : -kInf;
+            got[j] += x == -kInf ? 0.f : __builtin_amdgcn_exp2f(x - shared[row]);
+        }
     }
-    received[bh * a.capacity + key] += got;
+#pragma unroll
+    for (int j = 0; j < kReceivedKeys / kCombineThreads; ++j)
+        if (key[j] >= 0) out[key[j]] = old[j] + got[j];
 }
 
 template <int DIM, int G, int WAVES>
@@ -347,13 +372,13 @@ int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
         if (a.chunks > 1 || a.chunk_tiles > kKv4ShortTiles) return launch_decode<DIM, G, 4>(a, grid, cols, stream);
-        return launch_decode<DIM, G, DIM == 256 ? 8 : 16>(a, grid, cols, stream);
+        return launch_decode<DIM, G, 8>(a, grid, cols, stream);
     });
 }
 
 int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream)
 {
-    const int64_t blocks = received ? (s.capacity + kCombineThreads - 1) / kCombineThreads : 0;
+    const int64_t blocks = received ? (s.capacity + kReceivedKeys - 1) / kReceivedKeys : 0;
     const dim3 grid((unsigned)((a.chunks > 1 ? a.n_new * a.share : 0) + blocks), (unsigned)a.kv_heads, (unsigned)a.batch);
     switch (s.dim) {
         case 64: hipLaunchKernelGGL(kv4_combine_kernel<64>, grid, dim3(kCombineThreads), 0, stream, a, received); break;

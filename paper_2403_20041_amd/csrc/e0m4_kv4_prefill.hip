@@ -47,12 +47,13 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 1 : 2) void kv4_prefill_ke
     const Kv4Span span = kv4_span(a, b, block_row, block_rows);
     const int unit0 = span.begin / kKeys + chunk * a.chunk_tiles, units_end = (span.end + kKeys - 1) / kKeys;
     const int unit1 = unit0 + a.chunk_tiles < units_end ? unit0 + a.chunk_tiles : units_end;
-    if (unit0 >= unit1 && a.chunks > 1) return;
-
     const int row = block_row + wave * 32 + col, query = kv4_query_of(a, row), at = span.length - span.count + query;
     const bool valid = row < rows && query < span.count;
     half8_t q[kSteps];
     const float factor = load_query_row<DIM, kSteps, 32>(a, b, h, valid ? row : 0, valid, 8 * kh, 16, q);
+    if (a.packed_q && chunk == 0 && row < rows)
+        keep_query_row<kSteps>(a, ((int64_t)b * a.kv_heads + h) * rows + row, DIM, valid, 8 * kh, 16, q, factor);
+    if (unit0 >= unit1 && a.chunks > 1) return;
     const Kv4Seen by_place = kv4_seen(a, span.length, at);
     // this wavefront's rows: what some of them see, and what all of them see by position
     const int wave_row = block_row + wave * 32, wave_rows = rows - wave_row < 32 ? rows - wave_row : 32;

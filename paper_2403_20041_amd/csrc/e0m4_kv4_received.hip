@@ -13,18 +13,12 @@ namespace {
 
 constexpr int kThreads = 512, kKeys = 256, kQueries = 64;
 
-struct RowMeta {
-    float factor, lse;
-    int from, to;
-};
-
 template <int DIM, int G>
 __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, float* __restrict__ received)
 {
     using L = Kv4<DIM, G>;
     constexpr int kSteps = DIM / 16, kStride = DIM + 8, kPerRow = DIM / 8, kPieces = kQueries * kPerRow / kThreads;
     __shared__ __attribute__((aligned(16))) half_t staged[2][kQueries * kStride];
-    __shared__ __attribute__((aligned(16))) RowMeta metas[2][kQueries];
     __shared__ float part[2][kKeys];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, kh = lane >> 5;
     const int set = wave & 3, half = wave >> 2, rows = a.n_new * a.share;
@@ -62,36 +56,25 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
         }
     }
 
+    // queries, an iteration ahead in registers; a lane's own factor and sum
     words4_t raw[kPieces];
-    float raw_lse[kPieces];
+    float2 meta, next_meta;
+    const half_t* packed = a.packed_q + bh * rows * DIM;
     auto load = [&](int row0) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int r = row0 + (t + i * kThreads) / kPerRow, query = kv4_query_of(a, r), head = h * a.share + r - query * a.share;
-            const uint16_t* p = static_cast<const uint16_t*>(a.q.data) + b * a.q.batch_ld + query * a.q.row_ld + head * a.q.head_ld;
-            raw[i] = r < rows && query < count ? *reinterpret_cast<const words4_t*>(p + t % kPerRow * 8) : words4_t{0, 0, 0, 0};
-            raw_lse[i] = r < rows && query < count ? a.lse[bh * rows + r] : kInf;
+            const int r = row0 + (t + i * kThreads) / kPerRow;
+            raw[i] = words4_t{0, 0, 0, 0};
+            if (r < rows) raw[i] = *reinterpret_cast<const words4_t*>(packed + (int64_t)r * DIM + t % kPerRow * 8);
         }
+        const int r = row0 + 32 * half + col;
+        next_meta = float2{0.f, kInf};
+        if (r < rows) next_meta = float2{a.factors[bh * rows + r], a.lse[bh * rows + r]};
     };
-    auto store = [&](int row0, int into) {
+    auto store = [&](int into) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int at = (t + i * kThreads) / kPerRow, r = row0 + at;
-            half8_t q;
-            float factor = kLog2E / __builtin_sqrtf((float)DIM);
-            if (a.bf16) {
-                const int e = bf16_row_exponent<1, kPerRow, 1>(&raw[i]);
-                q = bf16_scaled(raw[i], e);
-                factor = __builtin_ldexpf(factor, e);
-            } else {
-                q = __builtin_bit_cast(half8_t, raw[i]);
-            }
-            *reinterpret_cast<half8_t*>(&staged[into][at * kStride + t % kPerRow * 8]) = q;
-            if (t % kPerRow == 0) {
-                const Kv4Seen s = kv4_seen(a, length, first + kv4_query_of(a, r));
-                metas[into][at] = RowMeta{factor, raw_lse[i], s.from, s.to};
-            }
-        }
+        for (int i = 0; i < kPieces; ++i)
+            *reinterpret_cast<words4_t*>(&staged[into][(t + i * kThreads) / kPerRow * kStride + t % kPerRow * 8]) = raw[i];
     };
 
     float got[2][16];
@@ -100,17 +83,19 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
 #pragma unroll
         for (int i = 0; i < 16; ++i) got[u][i] = 0.f;
     load(begin);
-    store(begin, 0);
-    if (begin + kQueries < end) load(begin + kQueries);
+    store(0);
+    meta = next_meta;
+    load(begin + kQueries);
     int at = 0;
     for (int row0 = begin; row0 < end; row0 += kQueries, at ^= 1) {
         __syncthreads();
-        if (row0 + kQueries < end) store(row0 + kQueries, at ^ 1);
-        if (row0 + 2 * kQueries < end) load(row0 + 2 * kQueries);
+        const float factor = meta.x, lse = meta.y;
+        meta = next_meta;
+        store(at ^ 1);
+        load(row0 + 2 * kQueries);
         const int mine = row0 + 32 * half;              // this wavefront's rows of queries
         const int q0 = kv4_query_of(a, mine), q1 = kv4_query_of(a, mine + 31);
         if (a.causal && first + q1 < own) continue;     // (they see none of its rows)
-        const RowMeta meta = metas[at][32 * half + col];
         const half_t* q = &staged[at][(32 * half + col) * kStride + 8 * kh];
         floatx16 s[2];
 #pragma unroll
@@ -138,19 +123,20 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
         }
         const bool some = a.mask || (a.causal && first + q0 + 1 < own + 64) || (a.window && first + q1 - a.window + 1 > own);
         if (some) {
+            const Kv4Seen by_place = kv4_seen(a, length, first + kv4_query_of(a, mine + col));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const bool in = row_of(u, i) >= meta.from && row_of(u, i) < meta.to && (seen >> (16 * u + i)) & 1;
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], meta.factor, -meta.lse));
+                    const bool in = row_of(u, i) >= by_place.from && row_of(u, i) < by_place.to && (seen >> (16 * u + i)) & 1;
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], factor, -lse));
                     got[u][i] += in ? e : 0.f;
                 }
         } else {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) got[u][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], meta.factor, -meta.lse));
+                for (int i = 0; i < 16; ++i) got[u][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], factor, -lse));
         }
     }
     // 32 sums over 32 lanes: at each step a lane gives away half of its sums and adds the other half of another's, until lane `col` has
@@ -162,8 +148,9 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
     for (int d = 16; d >= 1; d >>= 1)
 #pragma unroll
         for (int i = 0; i < d; ++i) {
-            const float keep = col & d ? v[i + d] : v[i], give = col & d ? v[i] : v[i + d];
-            v[i] = keep + __shfl_xor(give, d);
+            float low = v[i], high = v[i + d];
+            asm volatile("" : "+v"(low), "+v"(high));   // (or the choice becomes one of an index that no register has)
+            v[i] = (col & d ? high : low) + __shfl_xor(col & d ? low : high, d);
         }
     part[half][64 * set + 32 * (col >> 4) + 8 * ((col >> 2) & 3) + 4 * kh + (col & 3)] = v[0];
     __syncthreads();
