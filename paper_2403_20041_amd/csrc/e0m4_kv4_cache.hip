@@ -12,10 +12,64 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kMost = 57344.0f;       // magnitude limit: scale stays under 65504, so that every value of a group is finite
 
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+
 __device__ inline float bf16_float(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
 
+// Eight values of a row and the range of them and 0.  NaN counts as 0 and magnitudes are cut at kMost: one comparison of the largest
+// magnitude's bits says whether there is anything to do.
+__device__ inline void row_values(const uint4& raw, int bf16, float (&x)[8], float& mn, float& mx)
+{
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    ushort2_t top = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2_t, w[j] & 0x7FFF7FFFu));
+    const uint32_t most = top[0] > top[1] ? top[0] : top[1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint16_t bits = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        x[j] = bf16 ? bf16_float(bits) : (float)bits_half(bits);
+    }
+    if (most > (bf16 ? 0x4760u : 0x7B00u)) {            // (57344 in either type)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = x[j] == x[j] ? x[j] : 0.f;
+            x[j] = x[j] < -kMost ? -kMost : x[j];
+            x[j] = x[j] > kMost ? kMost : x[j];
+        }
+    }
+    mn = mx = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        mn = fminf(fminf(mn, x[j]), x[j + 1]);
+        mx = fmaxf(fmaxf(mx, x[j]), x[j + 1]);
+    }
+}
+
+// encode_value of two finite values at once, in 16-bit halves: the image's bits plus half a code's step, at most the binade's last, have
+// the code in fraction bits 9..6 (a step is 64 of them; the fifth fraction bit carries).
+__device__ inline uint32_t encode_pair(float a, float b, const Divisor& sf, float bf)
+{
+    float t[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float w = i ? b : a, q0 = w * sf.r;
+        const float q = __builtin_fmaf(__builtin_fmaf(-q0, sf.d, w), sf.r, q0);
+        t[i] = __builtin_amdgcn_fmed3f(q + bf, kLo, kHi);
+    }
+    const half2_t image = {(half_t)t[0], (half_t)t[1]};
+    ushort2_t bits = __builtin_bit_cast(ushort2_t, image) + (ushort2_t){32, 32};
+    bits = __builtin_elementwise_min(bits, (ushort2_t){0x43FF, 0x43FF});
+    return __builtin_bit_cast(uint32_t, bits) & kFracMask2;
+}
+// A word from four pairs of codes in fraction bits 9..6 (the inverse of the packed layout's shifts).
+__device__ inline uint32_t word_of_pairs(uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3)
+{
+    return p0 | (p1 >> 4) | (p2 << 4) | __builtin_amdgcn_alignbit(p3, p3, 24);
+}
+
 // One workgroup per tile of the cache that the new rows touch.  A row is DIM / 8 neighbouring threads with 8 values each; a group is
-// G / 8 lanes, its range is found among them.  A thread's eight K codes are one word of the layout.  V codes go through LDS, a byte
+// G / 8 lanes, its range is found among them.  A thread's eight K codes are one word of the layout.  V codes go through LDS, 16 bits
 // each, because a word of V holds eight rows; a word that also holds rows which stay is read and merged.
 template <int DIM, int G>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restrict__ cache, int64_t capacity, int64_t tiles, Kv4Rows keys,
@@ -23,8 +77,9 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
                                                               const int* __restrict__ counts)
 {
     using L = Kv4<DIM, G>;
-    constexpr int kPerRow = DIM / 8, kRowsAtOnce = kThreads / kPerRow;
-    __shared__ __attribute__((aligned(16))) uint8_t vcode[kKv4Rows][DIM];
+    constexpr int kPerRow = DIM / 8, kRowsAtOnce = kThreads / kPerRow, kTimes = kKv4Rows / kRowsAtOnce;
+    __shared__ __attribute__((aligned(16))) uint16_t vcode[kKv4Rows][DIM];   // (each in the fraction bits that it has in a pair)
+    __shared__ __attribute__((aligned(16))) uint32_t pieces[DIM][4];
     const int b = blockIdx.z, h = blockIdx.y, t = threadIdx.x;
     const int64_t start = starts[b];
     const int64_t end = start + (counts ? clamp_count(counts[b], n_new) : n_new);
@@ -36,27 +91,27 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
     if (lo >= hi) return;
     uint8_t* out = cache + (((int64_t)b * gridDim.y + h) * tiles + tile) * L::kBytes;
     const int p = t % kPerRow, r0 = t / kPerRow;
+    uint4 raw[2][kTimes];                               // (all rows are on their way before the first one's codes)
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        const Kv4Rows& src = v ? values : keys;
-        const uint16_t* base = static_cast<const uint16_t*>(src.data) + b * src.batch_ld + h * src.head_ld + 8 * p;
-        for (int r = r0; r < kKv4Rows; r += kRowsAtOnce) {
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const Kv4Rows& src = v ? values : keys;
+            const int r = r0 + i * kRowsAtOnce;
+            raw[v][i] = uint4{0, 0, 0, 0};
+            if (r >= lo && r < hi)
+                raw[v][i] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(src.data) + b * src.batch_ld + h * src.head_ld + 8 * p +
+                                                            (row0 + r - start) * src.row_ld);
+        }
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int r = r0 + i * kRowsAtOnce;
             if (r < lo || r >= hi) continue;            // (all lanes of a row alike)
-            const uint4 raw = *reinterpret_cast<const uint4*>(base + (row0 + r - start) * src.row_ld);
-            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
             float x[8];
-            float mn = 0.f, mx = 0.f;                   // the range always contains 0
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint16_t bits = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-                float f = bf16 ? bf16_float(bits) : (float)bits_half(bits);
-                f = f == f ? f : 0.f;
-                f = f < -kMost ? -kMost : f;
-                f = f > kMost ? kMost : f;
-                x[j] = f;
-                mn = fminf(mn, f);
-                mx = fmaxf(mx, f);
-            }
+            float mn, mx;
+            row_values(raw[v][i], bf16, x, mn, mx);
             group_range<G / 8>(mn, mx);
             float s = (mx - mn) / kSpan;
             s = s < kMinScale ? kMinScale : s;
@@ -67,54 +122,62 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
             z = z < kLo ? kLo : z;
             z = z > kHi ? kHi : z;
             const half_t bh = bits_half(half_bits((half_t)z) & 0xFFC0u);
-            uint32_t word = 0;
-            uint64_t bytes = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t c = encode_value(x[j], sf, (float)bh);
-                word |= place_code(c, j);
-                bytes |= (uint64_t)c << (8 * j);
-            }
             const bool writes = p % (G / 8) == 0;       // one lane for the group's parameters
             const int g = 8 * p / G;
+            uint32_t c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[j] = encode_pair(x[2 * j], x[2 * j + 1], sf, (float)bh);
             if (v == 0) {
-                *reinterpret_cast<uint32_t*>(out + L::k_word(r, 8 * p)) = word;
+                *reinterpret_cast<uint32_t*>(out + L::k_word(r, 8 * p)) = word_of_pairs(c[0], c[1], c[2], c[3]);
                 if (writes) *reinterpret_cast<uint32_t*>(out + L::k_param(r, g)) = (uint32_t)half_bits(sh) | ((uint32_t)half_bits(bh) << 16);
             } else {
-                *reinterpret_cast<uint64_t*>(&vcode[r][8 * p]) = bytes;
+                *reinterpret_cast<uint4*>(&vcode[r][8 * p]) = uint4{c[0], c[1], c[2], c[3]};
                 if (writes) {
                     *reinterpret_cast<uint16_t*>(out + L::v_param(r, g)) = half_bits(sh);
                     *reinterpret_cast<uint16_t*>(out + L::v_param(r, g) + 64) = half_bits(bh);
                 }
             }
         }
+    __syncthreads();
+    // V: four neighbouring dims of an octet per thread make a word each of four pieces
+    if (t < DIM) {
+        const int kq = t / (DIM / 4), d0 = t % (DIM / 4) * 4;
+        uint32_t pair[4][4];                            // [dim][slots 2 i, 2 i + 1]
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint2 four[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = L::row_of(kq, 2 * i + j);
+                four[j] = uint2{0, 0};
+                if (r >= lo && r < hi) four[j] = *reinterpret_cast<const uint2*>(&vcode[r][d0]);
+            }
+            pair[0][i] = __builtin_amdgcn_perm(four[1].x, four[0].x, 0x05040100u);
+            pair[1][i] = __builtin_amdgcn_perm(four[1].x, four[0].x, 0x07060302u);
+            pair[2][i] = __builtin_amdgcn_perm(four[1].y, four[0].y, 0x05040100u);
+            pair[3][i] = __builtin_amdgcn_perm(four[1].y, four[0].y, 0x07060302u);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pieces[d0 / 64 * 64 + kq * 16 + d0 % 16 + i][d0 % 64 / 16] = word_of_pairs(pair[i][0], pair[i][1], pair[i][2], pair[i][3]);
     }
     __syncthreads();
-    if (t >= DIM) return;                               // a piece of V per thread
-    const int kq = (t >> 4) & 3, d0 = (t >> 6) * 64 + (t & 15);
-    uint32_t stay = 0, word[4] = {0, 0, 0, 0};
-    bool any = false;
+    if (t >= DIM) return;
+    const int kq = (t >> 4) & 3;
+    uint32_t stay = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int r = L::row_of(kq, j);
-        if (r >= lo && r < hi) {
-            any = true;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) word[w] |= place_code(vcode[r][d0 + 16 * w], j);
-        } else {
-            stay |= place_code(15u, j);
-        }
+        if (r < lo || r >= hi) stay |= place_code(15u, j);
     }
-    if (!any) return;
+    if (stay == ~0u) return;
     uint4* dst = reinterpret_cast<uint4*>(out + L::kVCodes) + t;
+    uint4 word = *reinterpret_cast<const uint4*>(pieces[t]);
     if (stay) {
         const uint4 old = *dst;
-        word[0] |= old.x & stay;
-        word[1] |= old.y & stay;
-        word[2] |= old.z & stay;
-        word[3] |= old.w & stay;
+        word = uint4{word.x | (old.x & stay), word.y | (old.y & stay), word.z | (old.z & stay), word.w | (old.w & stay)};
     }
-    *dst = uint4{word[0], word[1], word[2], word[3]};
+    *dst = word;
 }
 
 // One workgroup per tile of the cache that the rows first ... first + rows - 1 touch: the codes' values go to LDS, whence rows are
@@ -196,14 +259,16 @@ __device__ inline uint32_t rank_bits(float f)
 
 // Which rows stay.  One workgroup per (sequence, head): the need-th largest weight of the old rows by four passes of 256 counters over
 // its bytes from the top, then one pass that counts and one that writes the rows above it, and the first ones that equal it, in
-// order; a wavefront has a contiguous part of the rows in both, so that places come from ballots and sixteen sums.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-__global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float* __restrict__ received, int64_t capacity,
+// order; a wavefront has a contiguous part of the rows in both, so that places come from ballots and sixteen sums.  Weights share
+// their upper bytes, so a counter is eight, one for every eighth lane.  The first kHeld weights stay in LDS after the first pass.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kCopies = 8, kHeld = 32768;
+__global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float* __restrict__ received, int64_t capacity, int held_most,
                                                                     const int* __restrict__ lengths, int budget, int recent,
                                                                     int* __restrict__ kept, int* __restrict__ lengths_out,
                                                                     float* __restrict__ received_out)
 {
-    __shared__ uint32_t count[256];
+    extern __shared__ float held[];
+    __shared__ __attribute__((aligned(16))) uint32_t count[256 * kCopies];
     __shared__ uint32_t found[2];                       // prefix of the threshold, rows still needed under it
     __shared__ int above[kSelectWaves], equal[kSelectWaves];
     const int b = blockIdx.y, h = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -226,26 +291,42 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
         ro[need + i] = w[old + i];
     }
     if (need == 0) return;
-    uint32_t prefix = 0, left = need;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = t; i < 256; i += kSelectThreads) count[i] = 0;
-        __syncthreads();
-        for (int i = t; i < old; i += kSelectThreads) {
-            const uint32_t u = rank_bits(w[i]);
-            if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&count[(u >> shift) & 255u], 1u);
+    const int in_lds = old < held_most ? old : held_most;
+    for (int i = t; i < 256 * kCopies; i += kSelectThreads) count[i] = 0;
+    __syncthreads();
+    constexpr int kAtOnce = 8;
+    for (int i0 = t; i0 < old; i0 += kAtOnce * kSelectThreads) {
+        float f[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) f[j] = i0 + j * kSelectThreads < old ? w[i0 + j * kSelectThreads] : 0.f;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int i = i0 + j * kSelectThreads;
+            if (i >= old) break;
+            if (i < in_lds) held[i] = f[j];
+            atomicAdd(&count[(rank_bits(f[j]) >> 24) * kCopies + (lane & (kCopies - 1))], 1u);
         }
+    }
+    uint32_t prefix = 0, left = need;
+    for (int shift = 24;; shift -= 8) {
         __syncthreads();
         if (wave == 0) {
-            // lane l has the counters 4 l .. 4 l + 3; rows at or above its last one, from the top
+            // lane l has the counters of 4 l .. 4 l + 3; rows above its last one, from the top
             uint32_t c[4], sum = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum += c[j] = count[4 * lane + j];
+            for (int j = 0; j < 4; ++j) {
+                const uint4* p = reinterpret_cast<const uint4*>(&count[(4 * lane + j) * kCopies]);
+                c[j] = (p[0].x + p[0].y) + (p[0].z + p[0].w) + (p[1].x + p[1].y) + (p[1].z + p[1].w);
+                sum += c[j];
+            }
             uint32_t upto = sum;
+#pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const uint32_t o = __shfl_down(upto, d);
                 if (lane + d < 64) upto += o;
             }
             uint32_t higher = upto - sum;
+#pragma unroll
             for (int j = 3; j >= 0; --j) {
                 if (higher < left && left <= higher + c[j]) {
                     found[0] = prefix | ((uint32_t)(4 * lane + j) << shift);
@@ -257,16 +338,28 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
         __syncthreads();
         prefix = found[0];
         left = found[1];
+        if (shift == 0) break;
+        for (int i = t; i < 256 * kCopies; i += kSelectThreads) count[i] = 0;
+        __syncthreads();
+        auto add = [&](uint32_t u) {
+            if ((u >> shift) == (prefix >> shift)) atomicAdd(&count[((u >> (shift - 8)) & 255u) * kCopies + (lane & (kCopies - 1))], 1u);
+        };
+#pragma unroll 4
+        for (int i = t; i < in_lds; i += kSelectThreads) add(rank_bits(held[i]));
+        for (int i = in_lds + t; i < old; i += kSelectThreads) add(rank_bits(w[i]));
     }
     const uint32_t threshold = prefix;                  // `left` rows that equal it stay
     const int part = ((old + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
     const int begin = wave * part, end = begin + part < old ? begin + part : old;
+    auto weight = [&](int i) { return i < in_lds ? held[i] : w[i]; };
     int na = 0, ne = 0;
+#pragma unroll 4
     for (int i = begin + lane; i < end; i += 64) {
-        const uint32_t u = rank_bits(w[i]);
+        const uint32_t u = rank_bits(weight(i));
         na += u > threshold;
         ne += u == threshold;
     }
+#pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         na += __shfl_xor(na, d);
         ne += __shfl_xor(ne, d);
@@ -284,8 +377,8 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
     const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
     for (int i0 = begin; i0 < end; i0 += 64) {
         const int i = i0 + lane;
-        const float f = i < end ? w[i] : 0.f;
-        const uint32_t u = i < end ? rank_bits(f) : 0u;
+        const float f = i < end ? weight(i) : 0.f;
+        const uint32_t u = rank_bits(f);
         const uint64_t ma = __ballot(i < end && u > threshold), me = __ballot(i < end && u == threshold);
         const int ea = e0 + __popcll(me & below), aa = a0 + __popcll(ma & below);
         const bool is_above = (ma >> lane) & 1, is_equal = (me >> lane) & 1;
@@ -302,7 +395,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
 // The rows that stay move to the smaller cache as they are.  One workgroup per tile of it: words of K are copied, words of V put
 // together from the eight rows' words.
 template <int DIM, int G>
-__global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const uint8_t* __restrict__ cache, int64_t tiles, const int* __restrict__ kept,
+__global__ __launch_bounds__(DIM) void kv4_gather_kernel(const uint8_t* __restrict__ cache, int64_t tiles, const int* __restrict__ kept,
                                                               int budget, uint8_t* __restrict__ small, int64_t small_tiles)
 {
     using L = Kv4<DIM, G>;
@@ -318,34 +411,40 @@ __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const uint8_t* __r
     const uint8_t* in = cache + bh * tiles * L::kBytes;
     uint8_t* out = small + (bh * small_tiles + blockIdx.x) * L::kBytes;
     auto tile_of = [&](int row) { return in + (int64_t)(row / kKv4Rows) * L::kBytes; };
-    if (t < DIM) {
-        {
-            const int r = t & 15, kq = (t >> 4) & 3, piece = t >> 6;
-            uint32_t word[4];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int s = DIM == 64 ? w >> 1 : piece / (DIM >= 128 ? DIM / 128 : 1);
-                const int lw = DIM == 64 ? w & 1 : piece % (DIM >= 128 ? DIM / 128 : 1) * 4 + w;
-                const int row = rows[16 * s + r];
-                word[w] = row < 0 ? 0u : *reinterpret_cast<const uint32_t*>(tile_of(row) + L::k_word(row % kKv4Rows, kq * L::kLaneDims + 8 * lw));
-            }
-            reinterpret_cast<uint4*>(out)[t] = uint4{word[0], word[1], word[2], word[3]};
+    const int kq = (t >> 4) & 3, block = t >> 6;        // a piece of K and one of V per thread
+    {
+        constexpr int kBlocks = DIM >= 128 ? DIM / 128 : 1;
+        uint4 piece = {0, 0, 0, 0};
+        if (DIM == 64) {
+            const int r0 = rows[t & 15], r1 = rows[16 + (t & 15)];
+            uint2 a = {0, 0}, c = {0, 0};
+            if (r0 >= 0) a = *reinterpret_cast<const uint2*>(tile_of(r0) + L::k_word(r0 % kKv4Rows, kq * L::kLaneDims));
+            if (r1 >= 0) c = *reinterpret_cast<const uint2*>(tile_of(r1) + L::k_word(r1 % kKv4Rows, kq * L::kLaneDims));
+            piece = uint4{a.x, a.y, c.x, c.y};
+        } else {
+            const int row = rows[16 * (block / kBlocks) + (t & 15)];
+            if (row >= 0) piece = *reinterpret_cast<const uint4*>(tile_of(row) + L::k_word(row % kKv4Rows, kq * L::kLaneDims + block % kBlocks * 32));
         }
-        const int kq = (t >> 4) & 3;
-        uint32_t word[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int row = rows[L::row_of(kq, j)];
-            if (row < 0) continue;
-            const int rr = row % kKv4Rows, from = L::slot(rr);
-            const uint4 raw = reinterpret_cast<const uint4*>(tile_of(row) + L::kVCodes)[(t & ~63) + L::octet(rr) * 16 + (t & 15)];
-            const uint32_t src[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) word[w] |= place_code(extract_code(src[w], from), j);
-        }
-        reinterpret_cast<uint4*>(out + L::kVCodes)[t] = uint4{word[0], word[1], word[2], word[3]};
+        reinterpret_cast<uint4*>(out)[t] = piece;
     }
-    for (int i = t; i < kKv4Rows * L::kGroups; i += kThreads) {
+    uint4 from[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int row = rows[L::row_of(kq, j)];
+        from[j] = uint4{0, 0, 0, 0};
+        if (row >= 0) from[j] = reinterpret_cast<const uint4*>(tile_of(row) + L::kVCodes)[block * 64 + L::octet(row % kKv4Rows) * 16 + (t & 15)];
+    }
+    uint32_t word[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int slot = L::slot(rows[L::row_of(kq, j)] & (kKv4Rows - 1));
+        const int shift = (0xE1 >> (slot >> 1 << 1) & 3) * 4 + 2 + (slot & 1) * 16;   // (nibble_shift: 6, 2, 10, 14 of a pair)
+        const uint32_t src[4] = {from[j].x, from[j].y, from[j].z, from[j].w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) word[w] |= place_code(__builtin_amdgcn_alignbit(src[w], src[w], shift), j);
+    }
+    reinterpret_cast<uint4*>(out + L::kVCodes)[t] = uint4{word[0], word[1], word[2], word[3]};
+    for (int i = t; i < kKv4Rows * L::kGroups; i += DIM) {
         const int r = i % kKv4Rows, g = i / kKv4Rows, row = rows[r];
         uint32_t kp = 0;
         uint16_t vs = 0, vb = 0;
@@ -392,14 +491,18 @@ int launch_kv4_read(const void* cache, const e0m4_kv4_shape& s, const int* lengt
 int launch_kv4_evict(const void* cache, const e0m4_kv4_shape& s, const float* received, const int* lengths, int budget, int recent,
                      void* small, const e0m4_kv4_shape& o, int* kept, int* lengths_out, float* received_out, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv4_select_kernel, dim3((unsigned)s.kv_heads, (unsigned)s.batch), dim3(kSelectThreads), 0, stream, received,
-                       s.capacity, lengths, budget, recent, kept, lengths_out, received_out);
-    const int rc = check_launch();
+    static std::atomic<uint64_t> allowed{0};
+    int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&kv4_select_kernel), kHeld * 4, allowed);
+    if (rc != E0M4_OK) return rc;
+    const int held = s.capacity < kHeld ? (int)s.capacity : kHeld;
+    hipLaunchKernelGGL(kv4_select_kernel, dim3((unsigned)s.kv_heads, (unsigned)s.batch), dim3(kSelectThreads), held * 4, stream, received,
+                       s.capacity, held, lengths, budget, recent, kept, lengths_out, received_out);
+    rc = check_launch();
     if (rc != E0M4_OK) return rc;
     const dim3 grid((unsigned)kv4_tiles(budget), (unsigned)s.kv_heads, (unsigned)s.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        hipLaunchKernelGGL((kv4_gather_kernel<DIM, G>), grid, dim3(kThreads), 0, stream, static_cast<const uint8_t*>(cache),
+        hipLaunchKernelGGL((kv4_gather_kernel<DIM, G>), grid, dim3(DIM), 0, stream, static_cast<const uint8_t*>(cache),
                            kv4_tiles(s.capacity), kept, budget, static_cast<uint8_t*>(small), kv4_tiles(o.capacity));
         return check_launch();
     });
