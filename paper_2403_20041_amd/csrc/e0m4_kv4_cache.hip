@@ -251,26 +251,27 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(const uint8_t* __res
 // Order of the received weights as an unsigned number: larger is more; -0 equals 0 and NaN counts as the most.
 __device__ inline uint32_t rank_bits(float f)
 {
-    const uint32_t u = __builtin_bit_cast(uint32_t, f + 0.0f);
-    if (f != f) return 0xFFFFFFFFu;
-    if (u == 0x80000000u) return 0x80000000u;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t u = __builtin_bit_cast(uint32_t, f + 0.0f);              // (-0 + 0 is 0)
+    return f != f ? 0xFFFFFFFFu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+__device__ inline float weight_of_rank(uint32_t r) { return __builtin_bit_cast(float, r & 0x80000000u ? r ^ 0x80000000u : ~r); }
 
-// Which rows stay.  One workgroup per (sequence, head): the need-th largest weight of the old rows by four passes of 256 counters over
-// its bytes from the top, then one pass that counts and one that writes the rows above it, and the first ones that equal it, in
-// order; a wavefront has a contiguous part of the rows in both, so that places come from ballots and sixteen sums.  Weights share
-// their upper bytes, so a counter is eight, one for every eighth lane.  The first kHeld weights stay in LDS after the first pass.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kCopies = 8, kHeld = 32768;
+// Which rows stay.  One workgroup per (sequence, head): the need-th largest weight of the old rows by three passes of up to 2048 counters
+// over its bits from the top, then one pass that counts and one that writes the rows above it, and the first ones that equal it, in
+// order; a wavefront has a contiguous part of the rows in both, so that places come from ballots and sixteen sums.  A counter is
+// four, one for every fourth lane: weights share their upper bits, and additions to one address follow each other.  After the
+// first pass the ranks of the first kHeld rows are in LDS.  What bounds it is arithmetic: one compute unit has a head's rows.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kHeld = 28672;
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float* __restrict__ received, int64_t capacity, int held_most,
                                                                     const int* __restrict__ lengths, int budget, int recent,
                                                                     int* __restrict__ kept, int* __restrict__ lengths_out,
                                                                     float* __restrict__ received_out)
 {
-    extern __shared__ float held[];
-    __shared__ __attribute__((aligned(16))) uint32_t count[256 * kCopies];
+    static_assert(kBins == 2 * kSelectThreads && kCopies == 4, "two counters of four copies per thread");
+    extern __shared__ uint32_t held[];
+    __shared__ __attribute__((aligned(16))) uint32_t count[kBins * kCopies];
     __shared__ uint32_t found[2];                       // prefix of the threshold, rows still needed under it
-    __shared__ int above[kSelectWaves], equal[kSelectWaves];
+    __shared__ uint32_t above[kSelectWaves], equal[kSelectWaves];
     const int b = blockIdx.y, h = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int64_t bh = (int64_t)b * gridDim.x + h;
     const float* w = received + bh * capacity;
@@ -286,13 +287,19 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
         return;
     }
     const int old = n - recent, need = budget - recent;     // need < old
-    for (int i = t; i < recent; i += kSelectThreads) {
-        k[need + i] = old + i;
-        ro[need + i] = w[old + i];
+    auto newest = [&]() {
+        for (int i = t; i < recent; i += kSelectThreads) {
+            k[need + i] = old + i;
+            ro[need + i] = w[old + i];
+        }
+    };
+    if (need == 0) {
+        newest();
+        return;
     }
-    if (need == 0) return;
     const int in_lds = old < held_most ? old : held_most;
-    for (int i = t; i < 256 * kCopies; i += kSelectThreads) count[i] = 0;
+    uint4* zero = reinterpret_cast<uint4*>(count) + 2 * t;
+    zero[0] = zero[1] = uint4{0, 0, 0, 0};
     __syncthreads();
     constexpr int kAtOnce = 8;
     for (int i0 = t; i0 < old; i0 += kAtOnce * kSelectThreads) {
@@ -303,93 +310,95 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
         for (int j = 0; j < kAtOnce; ++j) {
             const int i = i0 + j * kSelectThreads;
             if (i >= old) break;
-            if (i < in_lds) held[i] = f[j];
-            atomicAdd(&count[(rank_bits(f[j]) >> 24) * kCopies + (lane & (kCopies - 1))], 1u);
+            const uint32_t u = rank_bits(f[j]);
+            if (i < in_lds) held[i] = u;
+            atomicAdd(&count[(u >> 21) * kCopies + (lane & (kCopies - 1))], 1u);
         }
     }
     uint32_t prefix = 0, left = need;
-    for (int shift = 24;; shift -= 8) {
+    const int shifts[3] = {21, 10, 0}, masks[3] = {2047, 2047, 1023};
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
         __syncthreads();
-        if (wave == 0) {
-            // lane l has the counters of 4 l .. 4 l + 3; rows above its last one, from the top
-            uint32_t c[4], sum = 0;
+        const uint4 lo = zero[0], hi = zero[1];         // counters 2 t and 2 t + 1
+        const uint32_t c0 = (lo.x + lo.y) + (lo.z + lo.w), c1 = (hi.x + hi.y) + (hi.z + hi.w);
+        uint32_t upto = c0 + c1;                        // rows in this lane's counters and those of the lanes above
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint4* p = reinterpret_cast<const uint4*>(&count[(4 * lane + j) * kCopies]);
-                c[j] = (p[0].x + p[0].y) + (p[0].z + p[0].w) + (p[1].x + p[1].y) + (p[1].z + p[1].w);
-                sum += c[j];
-            }
-            uint32_t upto = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_down(upto, d);
-                if (lane + d < 64) upto += o;
-            }
-            uint32_t higher = upto - sum;
-#pragma unroll
-            for (int j = 3; j >= 0; --j) {
-                if (higher < left && left <= higher + c[j]) {
-                    found[0] = prefix | ((uint32_t)(4 * lane + j) << shift);
-                    found[1] = left - higher;
-                }
-                higher += c[j];
-            }
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_down(upto, d);
+            upto += lane + d < 64 ? o : 0u;
+        }
+        if (lane == 0) above[wave] = upto;
+        zero[0] = zero[1] = uint4{0, 0, 0, 0};
+        __syncthreads();
+        uint32_t higher = upto - (c0 + c1);
+        for (int i = wave + 1; i < kSelectWaves; ++i) higher += above[i];
+        if (higher < left && left <= higher + c1) {
+            found[0] = prefix | (uint32_t)(2 * t + 1) << shifts[pass];
+            found[1] = left - higher;
+        }
+        higher += c1;
+        if (higher < left && left <= higher + c0) {
+            found[0] = prefix | (uint32_t)(2 * t) << shifts[pass];
+            found[1] = left - higher;
         }
         __syncthreads();
         prefix = found[0];
         left = found[1];
-        if (shift == 0) break;
-        for (int i = t; i < 256 * kCopies; i += kSelectThreads) count[i] = 0;
-        __syncthreads();
+        if (pass == 2) break;
         auto add = [&](uint32_t u) {
-            if ((u >> shift) == (prefix >> shift)) atomicAdd(&count[((u >> (shift - 8)) & 255u) * kCopies + (lane & (kCopies - 1))], 1u);
+            if ((u ^ prefix) >> shifts[pass] == 0)
+                atomicAdd(&count[((u >> shifts[pass + 1]) & masks[pass + 1]) * kCopies + (lane & (kCopies - 1))], 1u);
         };
 #pragma unroll 4
-        for (int i = t; i < in_lds; i += kSelectThreads) add(rank_bits(held[i]));
+        for (int i = t; i < in_lds; i += kSelectThreads) add(held[i]);
         for (int i = in_lds + t; i < old; i += kSelectThreads) add(rank_bits(w[i]));
     }
     const uint32_t threshold = prefix;                  // `left` rows that equal it stay
     const int part = ((old + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
     const int begin = wave * part, end = begin + part < old ? begin + part : old;
-    auto weight = [&](int i) { return i < in_lds ? held[i] : w[i]; };
-    int na = 0, ne = 0;
+    auto place = [&](auto rank) {
+        uint32_t na = 0, ne = 0;
 #pragma unroll 4
-    for (int i = begin + lane; i < end; i += 64) {
-        const uint32_t u = rank_bits(weight(i));
-        na += u > threshold;
-        ne += u == threshold;
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        na += __shfl_xor(na, d);
-        ne += __shfl_xor(ne, d);
-    }
-    if (lane == 0) {
-        above[wave] = na;
-        equal[wave] = ne;
-    }
-    __syncthreads();
-    int a0 = 0, e0 = 0;
-    for (int i = 0; i < wave; ++i) {
-        a0 += above[i];
-        e0 += equal[i];
-    }
-    const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const float f = i < end ? weight(i) : 0.f;
-        const uint32_t u = rank_bits(f);
-        const uint64_t ma = __ballot(i < end && u > threshold), me = __ballot(i < end && u == threshold);
-        const int ea = e0 + __popcll(me & below), aa = a0 + __popcll(ma & below);
-        const bool is_above = (ma >> lane) & 1, is_equal = (me >> lane) & 1;
-        if (is_above || (is_equal && ea < (int)left)) {
-            const int at = aa + (ea < (int)left ? ea : (int)left);
-            k[at] = i;
-            ro[at] = f;
+        for (int i = begin + lane; i < end; i += 64) {
+            const uint32_t u = rank(i);
+            na += u > threshold;
+            ne += u == threshold;
         }
-        a0 += __popcll(ma);
-        e0 += __popcll(me);
-    }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            na += __shfl_xor(na, d);
+            ne += __shfl_xor(ne, d);
+        }
+        if (lane == 0) {
+            above[wave] = na;
+            equal[wave] = ne;
+        }
+        __syncthreads();
+        uint32_t a0 = 0, e0 = 0;
+        for (int i = 0; i < wave; ++i) {
+            a0 += above[i];
+            e0 += equal[i];
+        }
+        for (int i0 = begin; i0 < end; i0 += 64) {
+            const int i = i0 + lane;
+            const uint32_t u = i < end ? rank(i) : 0u;
+            const uint64_t ma = __ballot(i < end && u > threshold), me = __ballot(i < end && u == threshold);
+            uint32_t e = __builtin_amdgcn_mbcnt_hi((uint32_t)(me >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)me, e0));
+            const uint32_t a = __builtin_amdgcn_mbcnt_hi((uint32_t)(ma >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ma, a0));
+            if (i < end && (u > threshold || (u == threshold && e < left))) {
+                const uint32_t at = a + (e < left ? e : left);
+                k[at] = i;
+                ro[at] = weight_of_rank(u);
+            }
+            a0 += __popcll(ma);
+            e0 += __popcll(me);
+        }
+    };
+    // (a load from memory in the loop would wait for its stores: both are counted together)
+    if (old <= in_lds) place([&](int i) { return held[i]; });
+    else place([&](int i) { return rank_bits(w[i]); });
+    newest();
 }
 
 // The rows that stay move to the smaller cache as they are.  One workgroup per tile of it: words of K are copied, words of V put
