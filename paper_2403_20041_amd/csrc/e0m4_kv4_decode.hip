@@ -8,6 +8,8 @@
 #include "e0m4_kv4_attention.h"
 #include "e0m4_host.h"
 
+#include <type_traits>
+
 namespace e0m4 {
 
 namespace {
@@ -101,13 +103,21 @@ __device__ inline uint32_t seen_rows(const Kv4Attention& a, int b, int row0, int
     return seen;
 }
 
-template <int DIM, int G, int WAVES>
+// What the rounding of P to fp16 leaves is multiplied too where the result is fp16, whose own rounding is no larger than that of the few
+// weights that make a short row: by a second product (kRestSecond), or, where there are at most eight rows of queries, in the upper
+// eight columns of the one that there is, which hold the same rows again (kRestColumns: 32 heads on 8, 32 sequences of up to 8192 rows,
+// 51 us; with a second product 56, with neither 50).
+enum Rest { kRestNone, kRestSecond, kRestColumns };
+
+template <int DIM, int G, int WAVES, Rest REST>
 __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 ? 3 : 4) void kv4_decode_kernel(Kv4Attention a)
 {
     using L = Kv4<DIM, G>;
     constexpr int kSteps = DIM / 32, kDimTiles = DIM / 16, kStride = DIM + 4;
     extern __shared__ __attribute__((aligned(16))) float shared[];          // [wave][column][DIM + 4], then the statistics
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 15, kq = lane >> 4;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), kq = lane >> 4;
+    const int col = REST == kRestColumns ? lane & 7 : lane & 15;
+    const bool upper = REST == kRestColumns && (lane & 8);
     // (chunks are rotated from head to head: with a multiple of eight of them each would be one XCD's everywhere, and the last ones,
     // which short sequences do not have, leave theirs idle)
     const int b = blockIdx.z, h = blockIdx.y, chunk = (blockIdx.x + blockIdx.y + blockIdx.z * gridDim.y) % a.chunks, row0 = blockIdx.x / a.chunks * kCols;
@@ -129,7 +139,7 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 
     const bool valid = col < cols && query < span.count;
     // (rows from the sequence's count on are read too, so that nobody waits for it; their results are not used)
     const Queries<DIM> qs = load_queries<DIM>(a, b, h, col < cols ? row0 + col : 0, col < cols, kq);
-    if (a.packed_q && chunk == 0 && col < cols)
+    if (a.packed_q && chunk == 0 && col < cols && !upper)
         keep_query_row<kSteps>(a, ((int64_t)b * a.kv_heads + h) * rows + row0 + col, DIM, valid, kq * (DIM / 4), 8, qs.q, qs.factor);
     if (tile0 >= tile1 && a.chunks > 1) return;                             // (the sum knows)
     const Kv4Seen by_place = kv4_seen(a, span.length, at);
@@ -149,6 +159,7 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 
 #pragma unroll
     for (int d = 0; d < kDimTiles; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
     float ref = -kInf, sum = 0.f;
+    const float take_off = upper ? -1.f : 0.f;
 
     for (; tile < tile1; tile += WAVES) {
         // (behind the last one there is no access to memory)
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 
                 for (int i = 0; i < 4; ++i) s[u][i] = (seen >> (4 * u + i)) & 1 ? s[u][i] : -kInf;
             if (r0 + kKv4Rows > span.length) clear_v<DIM, G>(v, r0, kq, span.length);
         }
-        if (a.scores && valid) {
+        if (a.scores && valid && !upper) {
             float* out = a.scores + (((int64_t)b * a.kv_heads + h) * rows + row0 + col) * (a.tiles * kKv4Rows) + r0 + 4 * kq;
             *reinterpret_cast<floatx4*>(out) = s[0] * qs.factor;
             *reinterpret_cast<floatx4*>(out + 16) = s[1] * qs.factor;
@@ -187,14 +198,16 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 
             for (int d = 0; d < kDimTiles; ++d) o[d] *= down;
         }
         const float minus = ref == -kInf ? 0.f : kShift - ref;
-        half8_t p;
+        half8_t p, rest;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], qs.factor, minus));
                 sum += e;
-                p[4 * u + i] = (half_t)e;
+                const half_t near = (half_t)e;
+                p[4 * u + i] = REST == kRestColumns ? (half_t)__builtin_fmaf((float)near, take_off, e) : near;
+                if (REST == kRestSecond) rest[4 * u + i] = (half_t)(e - (float)near);
             }
 #pragma unroll
         for (int pc = 0; pc < L::kPieces; ++pc) {
@@ -202,17 +215,24 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 
             for (int w = 0; w < 4; ++w) {
                 const int g = (64 * pc + 16 * w) / G;
                 const Kv4OctetParams par = kv4_octet_params(v.scale[g], v.bias[g]);
-                o[4 * pc + w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv4_values_v(v.code[pc][w], par, hi, lo), p, o[4 * pc + w], 0, 0, 0);
+                const half8_t values = kv4_values_v(v.code[pc][w], par, hi, lo);
+                o[4 * pc + w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, p, o[4 * pc + w], 0, 0, 0);
+                if (REST == kRestSecond) o[4 * pc + w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, rest, o[4 * pc + w], 0, 0, 0);
             }
         }
         load_v(next, lane, v);
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    if (REST == kRestColumns)
+#pragma unroll
+        for (int d = 0; d < kDimTiles; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] += other_lane<0x128>(o[d][i]);      // (eight lanes on in the row of 16)
 
     // the wavefronts' results, in their order
     float* stats = shared + WAVES * cols * kStride;                         // [wave][column] reference, then sum
-    if (col < cols) {
+    if (col < cols && !upper) {
         float* mine = shared + (wave * cols + col) * kStride + 4 * kq;
 #pragma unroll
         for (int d = 0; d < kDimTiles; ++d) *reinterpret_cast<floatx4*>(mine + 16 * d) = o[d];
@@ -351,14 +371,14 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
         if (key[j] >= 0) out[key[j]] = old[j] + got[j];
 }
 
-template <int DIM, int G, int WAVES>
+template <int DIM, int G, int WAVES, Rest REST>
 int launch_decode(const Kv4Attention& a, dim3 grid, int cols, hipStream_t stream)
 {
     const int lds = (WAVES * cols * (DIM + 4) + 2 * WAVES * kCols) * 4;
     static std::atomic<uint64_t> allowed{0};
-    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&kv4_decode_kernel<DIM, G, WAVES>), 160 * 1024, allowed);
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&kv4_decode_kernel<DIM, G, WAVES, REST>), 160 * 1024, allowed);
     if (rc != E0M4_OK) return rc;
-    hipLaunchKernelGGL((kv4_decode_kernel<DIM, G, WAVES>), grid, dim3(WAVES * 64), lds, stream, a);
+    hipLaunchKernelGGL((kv4_decode_kernel<DIM, G, WAVES, REST>), grid, dim3(WAVES * 64), lds, stream, a);
     return check_launch();
 }
 
@@ -371,8 +391,13 @@ int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_
     const dim3 grid((unsigned)(row_tiles * a.chunks), (unsigned)a.kv_heads, (unsigned)a.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        if (a.chunks > 1 || a.chunk_tiles > kKv4ShortTiles) return launch_decode<DIM, G, 4>(a, grid, cols, stream);
-        return launch_decode<DIM, G, 8>(a, grid, cols, stream);
+        const bool shared = a.chunks > 1 || a.chunk_tiles > kKv4ShortTiles;
+        auto launch = [&](auto rest) -> int {
+            constexpr Rest REST = decltype(rest)::value;
+            return shared ? launch_decode<DIM, G, 4, REST>(a, grid, cols, stream) : launch_decode<DIM, G, 8, REST>(a, grid, cols, stream);
+        };
+        if (a.bf16) return launch(std::integral_constant<Rest, kRestNone>{});
+        return cols <= 8 ? launch(std::integral_constant<Rest, kRestColumns>{}) : launch(std::integral_constant<Rest, kRestSecond>{});
     });
 }
 
