@@ -43,6 +43,25 @@ struct Plan {
     size_t out_bytes, stats_bytes, lse_bytes, scores_bytes, queries_bytes;
     size_t bytes() const { return out_bytes + stats_bytes + lse_bytes + scores_bytes + queries_bytes; }
 };
+// Chunks of the cache for many queries.  A workgroup takes about 1.6 us for 64 rows of 128 dims when it is one of few (one head's 16 tokens
+// of 1001, their longest chain 16 times that, 28 us), the device 1.05 us for as many when it is full; partial results go to memory
+// and back, and the launch that adds them takes 4 us at least.
+int64_t prefill_chunks(const e0m4_kv4_shape& s, int64_t n_new, int64_t rows, int64_t sets, int64_t units)
+{
+    const double unit = s.dim / 128.0, seen = n_new < s.capacity ? 1.0 - 0.5 * n_new / s.capacity : 0.5;
+    const double full = sets * units * seen * 1.05 * unit / 256;
+    double best = 0;
+    int64_t chunks = 1;
+    for (int64_t c = 1; c <= 64 && c <= units; ++c) {
+        const double chain = (double)((units + c - 1) / c) * 1.6 * unit;
+        const double time = (chain > full ? chain : full) + (c > 1 ? 4.0 + c * (double)rows * s.dim * 8 / 3.5e6 : 0.0);
+        if (c == 1 || time < best) {
+            best = time;
+            chunks = c;
+        }
+    }
+    return chunks;
+}
 Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool weights)
 {
     Plan p;
@@ -55,15 +74,14 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     int64_t chunk;
     if (p.prefill) {
         p.tile_rows = s.dim == 128 && (force ? force == 3 : sets(256) >= 256 && 2 * n_new <= s.capacity) ? 256 : 128;
-        const int64_t n = sets(p.tile_rows);
-        chunk = n > 128 ? tiles : (tiles + 256 / n - 1) / (256 / n);
+        const int64_t n = prefill_chunks(s, n_new, all, sets(p.tile_rows), tiles);
+        chunk = (tiles + n - 1) / n;
     } else {
         p.tile_rows = 16;
         chunk = tiles * sets(16) / 3072;
         if (chunk < 8) chunk = 8;
         if (tiles <= kKv4ShortTiles) chunk = tiles;
     }
-    if (chunk < 4) chunk = 4;
     if (knob(Knob::kv4_chunk) > 0) chunk = knob(Knob::kv4_chunk);
     if (chunk < (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks) chunk = (tiles + kKv4MaxChunks - 1) / kKv4MaxChunks;
     if (chunk > tiles) chunk = tiles;

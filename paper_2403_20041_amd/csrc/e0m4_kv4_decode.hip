@@ -292,46 +292,39 @@ __device__ inline int chunks_of(const Kv4Attention& a, int b, int row, int rows,
     return (tiles + a.chunk_tiles - 1) / a.chunk_tiles;
 }
 
-// The sum over chunks, one workgroup per (sequence, head, row): a wavefront works out what they count for, then a thread has four dims
-// of every kParts-th chunk.  Workgroups beyond the rows' add what 2048 rows of the cache received, from the scores (tiles of 16 rows
-// of queries, one of them at most).
-constexpr int kCombineThreads = 256, kReceivedRows = 16, kReceivedKeys = 2048;
+// The sum over chunks, a wavefront per row: it works out what they count for, then its lanes take four dims of one chunk after the other
+// (of two or four chunks at a time where a row is shorter than 64 such pieces).  Workgroups beyond the rows' add what 2048 rows of
+// the cache received, from the scores (tiles of 16 rows of queries, one of them at most).
+constexpr int kCombineThreads = 256, kCombineRows = kCombineThreads / 64, kReceivedRows = 16, kReceivedKeys = 2048;
+__host__ __device__ inline int combine_sums(const Kv4Attention& a) { return a.chunks > 1 ? (a.n_new * a.share + kCombineRows - 1) / kCombineRows : 0; }
 template <int DIM>
 __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attention a, float* __restrict__ received)
 {
-    constexpr int kPer = DIM / 4, kParts = kCombineThreads / kPer;
-    __shared__ float factor[kKv4MaxChunks];
-    __shared__ floatx4 part[kParts][kPer];
+    constexpr int kPer = DIM / 4, kAtOnce = 64 / kPer;
+    __shared__ float factors[kCombineRows][kKv4MaxChunks];
     __shared__ float shared[kReceivedRows];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = blockIdx.y, b = blockIdx.z, rows = a.n_new * a.share;
     const int64_t stride = (int64_t)a.batch * a.kv_heads * rows, bh = (int64_t)b * a.kv_heads + h;
-    const int sums = a.chunks > 1 ? rows : 0;
+    const int sums = combine_sums(a);
     Kv4Span span;
     if ((int)blockIdx.x < sums) {
-        const int row = blockIdx.x, chunks = chunks_of(a, b, row, rows, span);
+        const int row = blockIdx.x * kCombineRows + wave;
+        if (row >= rows) return;
+        const int chunks = chunks_of(a, b, row, rows, span);
         const int64_t at = bh * rows + row;
-        float top, total;
-        if (wave == 0) {
-            total = chunk_factors(a.part_stats + at, stride, chunks, lane, top, factor);
-            if (lane == 0) {
-                shared[0] = top;
-                shared[1] = total;
-            }
-        }
-        __syncthreads();
-        top = shared[0];
-        total = shared[1];
-        const int d = t % kPer * 4, q = t / kPer;
+        float* factor = factors[wave];
+        float top;
+        const float total = chunk_factors(a.part_stats + at, stride, chunks, lane, top, factor);
+        const int d = lane % kPer * 4;
         const float* p = a.part_out + at * DIM + d;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int c = q; c < chunks; c += kParts) acc += *reinterpret_cast<const floatx4*>(p + c * stride * DIM) * factor[c];
-        part[q][t % kPer] = acc;
-        __syncthreads();
-        if (q) return;
+#pragma unroll 8
+        for (int c = lane / kPer; c < chunks; c += kAtOnce) acc += *reinterpret_cast<const floatx4*>(p + c * stride * DIM) * factor[c];
 #pragma unroll
-        for (int i = 1; i < kParts; ++i) acc += part[i][t];
-        finish<DIM>(a, b, h, row, d, kv4_query_of(a, row) < span.count, acc, top, total);
+        for (int s = kPer; s < 64; s <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], s);
+        if (lane < kPer) finish<DIM>(a, b, h, row, d, kv4_query_of(a, row) < span.count, acc, top, total);
         return;
     }
     const int chunks = chunks_of(a, b, 0, rows, span), key0 = ((int)blockIdx.x - sums) * kReceivedKeys;
@@ -404,7 +397,7 @@ int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_
 int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream)
 {
     const int64_t blocks = received ? (s.capacity + kReceivedKeys - 1) / kReceivedKeys : 0;
-    const dim3 grid((unsigned)((a.chunks > 1 ? a.n_new * a.share : 0) + blocks), (unsigned)a.kv_heads, (unsigned)a.batch);
+    const dim3 grid((unsigned)(combine_sums(a) + blocks), (unsigned)a.kv_heads, (unsigned)a.batch);
     switch (s.dim) {
         case 64: hipLaunchKernelGGL(kv4_combine_kernel<64>, grid, dim3(kCombineThreads), 0, stream, a, received); break;
         case 128: hipLaunchKernelGGL(kv4_combine_kernel<128>, grid, dim3(kCombineThreads), 0, stream, a, received); break;
