@@ -141,7 +141,9 @@ struct Kv4Attention {
     int tile_rows, tile_keys;                           // rows of queries that go through the cache together, rows of it at a time
     float* part_out;                                    // [chunk][batch][kv_heads][rows][dim]
     float2* part_stats;                                 // [chunk][batch][kv_heads][rows]: reference exponent, sum
-    float* lse;                                         // [batch][kv_heads][rows] log2 of the softmax's sum, for the received weights
+    // for the received weights: [batch][kv_heads][rows] reference exponent and what 2^(score - reference) counts for (zero in rows that see
+    // nothing).  A log2 of the sum would do in one number, but its rounding is that of a score's whole size.
+    float2* norm;
     half_t* packed_q;                                   // [batch][kv_heads][rows][dim] queries as the products take them, and
     float* factors;                                     // [batch][kv_heads][rows] their scores' factors, or null
     float* scores;                                      // [batch][kv_heads][rows][tiles * 32] in powers of two, or null

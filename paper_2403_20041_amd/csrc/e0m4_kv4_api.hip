@@ -40,8 +40,8 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 struct Plan {
     bool prefill, scores;
     int tile_rows, tile_keys, chunk_tiles, chunks;
-    size_t out_bytes, stats_bytes, lse_bytes, scores_bytes, queries_bytes;
-    size_t bytes() const { return out_bytes + stats_bytes + lse_bytes + scores_bytes + queries_bytes; }
+    size_t out_bytes, stats_bytes, norm_bytes, scores_bytes, queries_bytes;
+    size_t bytes() const { return out_bytes + stats_bytes + norm_bytes + scores_bytes + queries_bytes; }
 };
 // Chunks of the cache for many queries.  A workgroup takes about 1.6 us for 64 rows of 128 dims when it is one of few (one head's 16 tokens
 // of 1001, their longest chain 16 times that, 28 us), the device 1.05 us for as many when it is full; partial results go to memory
@@ -67,7 +67,12 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     Plan p;
     const int64_t rows = heads / s.kv_heads * n_new, all = s.batch * s.kv_heads * rows;
     const int force = knob(Knob::kv4_attention);
-    p.prefill = force ? force >= 2 : rows > 32;
+    // The kernel for few queries dequantises the cache again for every 16 rows of them, the other one shares it among 128, but has longer
+    // chains and leaves a workgroup's missing rows idle.  8 sequences of 3000 rows and 8 heads, us of the two: 49 rows of queries 31
+    // and 29, 97 rows 42 and 38, 33 rows 24 and 27; 500 rows, 129 rows of queries 14 and 21; 16 sequences of 500 rows and 8 heads, 193
+    // rows of queries (36608 tiles taken) 22 and 18, one of 16000 and 2 heads (13026) 29 and 25, of 3000 (2470) 15 and 18.
+    const int64_t taken = (s.capacity + kKv4Rows - 1) / kKv4Rows * s.batch * s.kv_heads * ((rows + 15) / 16);
+    p.prefill = force ? force >= 2 : rows > 64 && taken > 12000;
     p.tile_keys = p.prefill ? kKv4PrefillKeys : kKv4Rows;
     const int64_t tiles = (s.capacity + p.tile_keys - 1) / p.tile_keys;
     auto sets = [&](int tile_rows) { return s.batch * s.kv_heads * ((rows + tile_rows - 1) / tile_rows); };
@@ -90,7 +95,7 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     p.scores = weights && !p.prefill && rows <= 16;
     p.out_bytes = p.chunks > 1 ? (size_t)p.chunks * all * s.dim * 4 : 0;
     p.stats_bytes = p.chunks > 1 ? round16((size_t)p.chunks * all * 8) : 0;
-    p.lse_bytes = weights ? round16((size_t)all * 4) : 0;
+    p.norm_bytes = weights ? round16((size_t)all * 8) : 0;
     p.queries_bytes = weights && !p.scores ? (size_t)all * s.dim * 2 + round16((size_t)all * 4) : 0;
     p.scores_bytes = p.scores ? (size_t)all * kv4_tiles(s.capacity) * kKv4Rows * 4 : 0;
     return p;
@@ -216,12 +221,12 @@ int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, i
     char* w = static_cast<char*>(workspace);
     a.part_out = reinterpret_cast<float*>(w);
     a.part_stats = reinterpret_cast<float2*>(w + p.out_bytes);
-    a.lse = weights ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes) : nullptr;
+    a.norm = weights ? reinterpret_cast<float2*>(w + p.out_bytes + p.stats_bytes) : nullptr;
     if (p.queries_bytes) {
-        a.packed_q = reinterpret_cast<half_t*>(w + p.out_bytes + p.stats_bytes + p.lse_bytes);
+        a.packed_q = reinterpret_cast<half_t*>(w + p.out_bytes + p.stats_bytes + p.norm_bytes);
         a.factors = reinterpret_cast<float*>(a.packed_q + (size_t)a.batch * heads * n_new * s->dim);
     }
-    a.scores = p.scores ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes + p.lse_bytes) : nullptr;
+    a.scores = p.scores ? reinterpret_cast<float*>(w + p.out_bytes + p.stats_bytes + p.norm_bytes) : nullptr;
     rc = p.prefill ? launch_kv4_prefill(a, *s, (hipStream_t)stream) : launch_kv4_decode(a, *s, (hipStream_t)stream);
     if (rc == E0M4_OK && (a.chunks > 1 || p.scores)) rc = launch_kv4_combine(a, *s, p.scores ? weights : nullptr, (hipStream_t)stream);
     if (rc == E0M4_OK && weights && !p.scores) rc = launch_kv4_received(a, *s, weights, (hipStream_t)stream);

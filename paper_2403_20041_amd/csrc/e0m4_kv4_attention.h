@@ -27,6 +27,13 @@ __device__ inline uint32_t bf16_round(float f)
     return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
 }
 
+// What a row's weights take from its reference and sum (of 2^(t - ref + kShift)).
+__device__ inline float2 row_norm(bool valid, float ref, float sum)
+{
+    return !valid || sum == 0.f ? float2{0.f, 0.f} : float2{ref, 256.f / sum};
+}
+static_assert(kShift == 8.f, "2^kShift over the sum");
+
 // Four dims of a row's result from its sums; zeros for a row that sees nothing.
 template <int DIM>
 __device__ inline void finish(const Kv4Attention& a, int b, int h, int row, int d, bool valid, floatx4 acc, float ref, float sum)
@@ -41,8 +48,7 @@ __device__ inline void finish(const Kv4Attention& a, int b, int h, int row, int 
         x[j] = a.bf16 ? bf16_round(y) : (uint32_t)__builtin_bit_cast(uint16_t, (half_t)y);
     }
     *reinterpret_cast<uint2*>(p) = uint2{x[0] | (x[1] << 16), x[2] | (x[3] << 16)};
-    if (a.lse && d == 0)
-        a.lse[((int64_t)b * a.kv_heads + h) * ((int64_t)a.n_new * a.share) + row] = f == 0.f ? kInf : ref - kShift + __builtin_amdgcn_logf(sum);
+    if (a.norm && d == 0) a.norm[((int64_t)b * a.kv_heads + h) * ((int64_t)a.n_new * a.share) + row] = row_norm(valid, ref, sum);
 }
 
 __device__ inline words4_t load16(__amdgpu_buffer_rsrc_t tile, int offset)

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
 {
     constexpr int kPer = DIM / 4, kAtOnce = 64 / kPer;
     __shared__ float factors[kCombineRows][kKv4MaxChunks];
-    __shared__ float shared[kReceivedRows];
+    __shared__ float2 norms[kReceivedRows];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = blockIdx.y, b = blockIdx.z, rows = a.n_new * a.share;
     const int64_t stride = (int64_t)a.batch * a.kv_heads * rows, bh = (int64_t)b * a.kv_heads + h;
     const int sums = combine_sums(a);
@@ -333,10 +333,10 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
         for (int row = wave; row < rows; row += kCombineThreads / 64) {
             float top;
             const float total = chunk_factors(a.part_stats + bh * rows + row, stride, chunks, lane, top, nullptr);
-            if (lane == 0) shared[row] = kv4_query_of(a, row) < span.count && total != 0.f ? top - kShift + __builtin_amdgcn_logf(total) : kInf;
+            if (lane == 0) norms[row] = row_norm(kv4_query_of(a, row) < span.count, top, total);
         }
     } else if (t < rows) {
-        shared[t] = a.lse[bh * rows + t];
+        norms[t] = a.norm[bh * rows + t];
     }
     __syncthreads();
     const int low = span.begin / kKv4Rows * kKv4Rows;
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
 #pragma unroll
         for (int j = 0; j < kReceivedKeys / kCombineThreads; ++j) {
             const float x = key[j] >= 0 ? s[row * (a.tiles * kKv4Rows) + key[j]] : -kInf;
-            got[j] += x == -kInf ? 0.f : __builtin_amdgcn_exp2f(x - shared[row]);
+            got[j] = x == -kInf ? got[j] : __builtin_fmaf(__builtin_amdgcn_exp2f(x - norms[row].x), norms[row].y, got[j]);
         }
     }
 #pragma unroll

@@ -1,5 +1,5 @@
-// What the rows of a cache in E0M4 codes received: received[j] += sum over rows of queries of 2^(score - lse), with the log2 sums that
-// the attention left.  Scores are formed a second time: kept from the first, they would take four bytes each, 8 / dim of the
+// What the rows of a cache in E0M4 codes received: received[j] += sum over rows of queries of 2^(score - reference) times what the
+// attention left for the row (e0m4_kv4.h, norm).  Scores are formed a second time: kept from the first, they would take four bytes each, 8 / dim of the
 // operations' time at the card's rates, twice.
 //
 // A workgroup owns 256 rows of the cache, so no two add to one number.  Four pairs of wavefronts hold 64 rows of K each as operands in
@@ -58,7 +58,8 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
 
     // queries, an iteration ahead in registers; a lane's own factor and sum
     words4_t raw[kPieces];
-    float2 meta, next_meta;
+    float factor, next_factor;
+    float2 norm, next_norm;
     const half_t* packed = a.packed_q + bh * rows * DIM;
     auto load = [&](int row0) {
 #pragma unroll
@@ -68,8 +69,12 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
             if (r < rows) raw[i] = *reinterpret_cast<const words4_t*>(packed + (int64_t)r * DIM + t % kPerRow * 8);
         }
         const int r = row0 + 32 * half + col;
-        next_meta = float2{0.f, kInf};
-        if (r < rows) next_meta = float2{a.factors[bh * rows + r], a.lse[bh * rows + r]};
+        next_factor = 0.f;
+        next_norm = float2{0.f, 0.f};
+        if (r < rows) {
+            next_factor = a.factors[bh * rows + r];
+            next_norm = a.norm[bh * rows + r];
+        }
     };
     auto store = [&](int into) {
 #pragma unroll
@@ -84,13 +89,15 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
         for (int i = 0; i < 16; ++i) got[u][i] = 0.f;
     load(begin);
     store(0);
-    meta = next_meta;
+    factor = next_factor;
+    norm = next_norm;
     load(begin + kQueries);
     int at = 0;
     for (int row0 = begin; row0 < end; row0 += kQueries, at ^= 1) {
         __syncthreads();
-        const float factor = meta.x, lse = meta.y;
-        meta = next_meta;
+        const float by = factor, ref = norm.x, weight = norm.y;
+        factor = next_factor;
+        norm = next_norm;
         store(at ^ 1);
         load(row0 + 2 * kQueries);
         const int mine = row0 + 32 * half;              // this wavefront's rows of queries
@@ -129,14 +136,14 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const bool in = row_of(u, i) >= by_place.from && row_of(u, i) < by_place.to && (seen >> (16 * u + i)) & 1;
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], factor, -lse));
-                    got[u][i] += in ? e : 0.f;
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], by, -ref));
+                    got[u][i] = in ? __builtin_fmaf(e, weight, got[u][i]) : got[u][i];
                 }
         } else {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) got[u][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], factor, -lse));
+                for (int i = 0; i < 16; ++i) got[u][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], by, -ref)), weight, got[u][i]);
         }
     }
     // 32 sums over 32 lanes: at each step a lane gives away half of its sums and adds the other half of another's, until lane `col` has
