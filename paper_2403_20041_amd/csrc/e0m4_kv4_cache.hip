@@ -5,6 +5,8 @@
 #include "e0m4_host.h"
 #include "e0m4_kv4.h"
 
+#include <type_traits>
+
 namespace e0m4 {
 
 namespace {
@@ -13,37 +15,64 @@ constexpr int kThreads = 256;
 constexpr float kMost = 57344.0f;       // magnitude limit: scale stays under 65504, so that every value of a group is finite
 
 typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+typedef short short2_t __attribute__((ext_vector_type(2)));
 
 __device__ inline float bf16_float(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
 
-// Eight values of a row and the range of them and 0.  NaN counts as 0 and magnitudes are cut at kMost: one comparison of the largest
-// magnitude's bits says whether there is anything to do.
-__device__ inline void row_values(const uint4& raw, int bf16, float (&x)[8], float& mn, float& mx)
+// Range of a group's values and 0, LANES neighbouring lanes with eight each: the largest value in the low half, the magnitude of the
+// smallest in the high one, as 16-bit patterns of the rows' own type, which order like signed integers where they are positive.
+// NaN counts as 0 and magnitudes are cut at kMost: patterns above its say whether there is anything to do.
+__device__ inline uint32_t pack_max(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2_t, a), __builtin_bit_cast(short2_t, b)));
+}
+template <int LANES>
+__device__ inline void group_values(const uint4& raw, int bf16, float (&x)[8], float& mn, float& mx)
 {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    ushort2_t top = {0, 0};
+    uint32_t up = 0, down = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2_t, w[j] & 0x7FFF7FFFu));
-    const uint32_t most = top[0] > top[1] ? top[0] : top[1];
+    for (int j = 0; j < 4; ++j) {
+        up = pack_max(up, w[j]);
+        down = pack_max(down, w[j] ^ 0x80008000u);
+    }
+    // both halves' largest: (up, down) of either
+    uint32_t range = pack_max(__builtin_amdgcn_perm(down, up, 0x05040100u), __builtin_amdgcn_perm(down, up, 0x07060302u));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint16_t bits = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
         x[j] = bf16 ? bf16_float(bits) : (float)bits_half(bits);
     }
-    if (most > (bf16 ? 0x4760u : 0x7B00u)) {            // (57344 in either type)
+    const uint32_t most = bf16 ? 0x4760u : 0x7B00u;     // 57344 in either type
+    if ((range & 0xFFFFu) > most || (range >> 16) > most) {
+        float low = 0.f, high = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             x[j] = x[j] == x[j] ? x[j] : 0.f;
             x[j] = x[j] < -kMost ? -kMost : x[j];
             x[j] = x[j] > kMost ? kMost : x[j];
+            low = fminf(low, x[j]);
+            high = fmaxf(high, x[j]);
         }
+        range = bf16 ? (__builtin_bit_cast(uint32_t, high) >> 16) | (__builtin_bit_cast(uint32_t, -low) & 0xFFFF0000u)
+                     : (uint32_t)half_bits((half_t)high) | ((uint32_t)half_bits((half_t)-low) << 16);
+        range &= 0x7FFF7FFFu;                           // (-0)
     }
-    mn = mx = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-        mn = fminf(fminf(mn, x[j]), x[j + 1]);
-        mx = fmaxf(fmaxf(mx, x[j]), x[j + 1]);
-    }
+    auto other = [](uint32_t v, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, true); };
+    range = pack_max(range, other(range, std::integral_constant<int, 0xB1>{}));             // (lanes as in group_range)
+    range = pack_max(range, other(range, std::integral_constant<int, 0x4E>{}));
+    if (LANES >= 8) range = pack_max(range, other(range, std::integral_constant<int, 0x141>{}));
+    if (LANES == 16) range = pack_max(range, other(range, std::integral_constant<int, 0x140>{}));
+    const uint16_t high = (uint16_t)range, low = (uint16_t)(range >> 16);
+    mx = bf16 ? bf16_float(high) : (float)bits_half(high);
+    mn = -(bf16 ? bf16_float(low) : (float)bits_half(low));
+}
+// The correctly rounded reciprocal of an fp16 number: from one within a unit in the last place, the remainder exact, one step (Markstein,
+// as cited at Divisor; it fails for a divisor whose 24 bits are all ones only).
+__device__ inline Divisor divisor_of_half(float d)
+{
+    const float r = __builtin_amdgcn_rcpf(d);
+    return Divisor{d, __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r)};
 }
 
 // encode_value of two finite values at once, in 16-bit halves: the image's bits plus half a code's step, at most the binade's last, have
@@ -111,16 +140,11 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
             if (r < lo || r >= hi) continue;            // (all lanes of a row alike)
             float x[8];
             float mn, mx;
-            row_values(raw[v][i], bf16, x, mn, mx);
-            group_range<G / 8>(mn, mx);
-            float s = (mx - mn) / kSpan;
-            s = s < kMinScale ? kMinScale : s;
-            s = s > kMaxScale ? kMaxScale : s;
-            const half_t sh = (half_t)s;
-            const Divisor sf = make_divisor((float)sh);
-            float z = kLo - quotient(mn, sf);
-            z = z < kLo ? kLo : z;
-            z = z > kHi ? kHi : z;
+            group_values<G / 8>(raw[v][i], bf16, x, mn, mx);
+            constexpr Divisor span = {kSpan, 1.0f / kSpan};                 // (what leaves quotient()'s range is below kMinScale)
+            const half_t sh = (half_t)__builtin_amdgcn_fmed3f(quotient(mx - mn, span), kMinScale, kMaxScale);
+            const Divisor sf = divisor_of_half((float)sh);
+            const float z = __builtin_amdgcn_fmed3f(kLo - quotient(mn, sf), kLo, kHi);
             const half_t bh = bits_half(half_bits((half_t)z) & 0xFFC0u);
             const bool writes = p % (G / 8) == 0;       // one lane for the group's parameters
             const int g = 8 * p / G;
