@@ -15,6 +15,7 @@ constexpr int kThreads = 256;
 constexpr float kMost = 57344.0f;       // magnitude limit: scale stays under 65504, so that every value of a group is finite
 
 typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
 typedef short short2_t __attribute__((ext_vector_type(2)));
 
 __device__ inline float bf16_float(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
@@ -26,8 +27,8 @@ __device__ inline uint32_t pack_max(uint32_t a, uint32_t b)
 {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2_t, a), __builtin_bit_cast(short2_t, b)));
 }
-template <int LANES>
-__device__ inline void group_values(const uint4& raw, int bf16, float (&x)[8], float& mn, float& mx)
+template <int LANES, bool bf16>
+__device__ inline void group_values(const uint4& raw, float (&x)[8], float& mn, float& mx)
 {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
     uint32_t up = 0, down = 0;
@@ -86,7 +87,7 @@ __device__ inline uint32_t encode_pair(float a, float b, const Divisor& sf, floa
         const float q = __builtin_fmaf(__builtin_fmaf(-q0, sf.d, w), sf.r, q0);
         t[i] = __builtin_amdgcn_fmed3f(q + bf, kLo, kHi);
     }
-    const half2_t image = {(half_t)t[0], (half_t)t[1]};
+    const half2_t image = __builtin_convertvector((float2_t){t[0], t[1]}, half2_t);
     ushort2_t bits = __builtin_bit_cast(ushort2_t, image) + (ushort2_t){32, 32};
     bits = __builtin_elementwise_min(bits, (ushort2_t){0x43FF, 0x43FF});
     return __builtin_bit_cast(uint32_t, bits) & kFracMask2;
@@ -100,9 +101,9 @@ __device__ inline uint32_t word_of_pairs(uint32_t p0, uint32_t p1, uint32_t p2, 
 // One workgroup per tile of the cache that the new rows touch.  A row is DIM / 8 neighbouring threads with 8 values each; a group is
 // G / 8 lanes, its range is found among them.  A thread's eight K codes are one word of the layout.  V codes go through LDS, 16 bits
 // each, because a word of V holds eight rows; a word that also holds rows which stay is read and merged.
-template <int DIM, int G>
+template <int DIM, int G, bool BF16>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restrict__ cache, int64_t capacity, int64_t tiles, Kv4Rows keys,
-                                                              Kv4Rows values, int bf16, int64_t n_new, const int* __restrict__ starts,
+                                                              Kv4Rows values, int64_t n_new, const int* __restrict__ starts,
                                                               const int* __restrict__ counts)
 {
     using L = Kv4<DIM, G>;
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
             if (r < lo || r >= hi) continue;            // (all lanes of a row alike)
             float x[8];
             float mn, mx;
-            group_values<G / 8>(raw[v][i], bf16, x, mn, mx);
+            group_values<G / 8, BF16>(raw[v][i], x, mn, mx);
             constexpr Divisor span = {kSpan, 1.0f / kSpan};                 // (what leaves quotient()'s range is below kMinScale)
             const half_t sh = (half_t)__builtin_amdgcn_fmed3f(quotient(mx - mn, span), kMinScale, kMaxScale);
             const Divisor sf = divisor_of_half((float)sh);
@@ -502,9 +503,12 @@ int launch_kv4_append(void* cache, const e0m4_kv4_shape& s, const Kv4Rows& keys,
     const dim3 grid((unsigned)touched, (unsigned)s.kv_heads, (unsigned)s.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        hipLaunchKernelGGL((kv4_append_kernel<DIM, G>), grid, dim3(kThreads), 0, stream, static_cast<uint8_t*>(cache), s.capacity, tiles,
-                           keys, values, dtype == E0M4_KV4_BF16, n_new, starts, counts);
-        return check_launch();
+        auto launch = [&](auto kernel) -> int {
+            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, static_cast<uint8_t*>(cache), s.capacity, tiles, keys, values, n_new,
+                               starts, counts);
+            return check_launch();
+        };
+        return dtype == E0M4_KV4_BF16 ? launch(&kv4_append_kernel<DIM, G, true>) : launch(&kv4_append_kernel<DIM, G, false>);
     });
 }
 
