@@ -78,10 +78,17 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     auto sets = [&](int tile_rows) { return s.batch * s.kv_heads * ((rows + tile_rows - 1) / tile_rows); };
     int64_t chunk;
     if (p.prefill) {
+        // 256 rows to a workgroup halve the dequantisation of 128, two workgroups of which a compute unit has at once: the larger ones where
+        // they fill the device with like work (2048 tokens behind 14336, 617 us against 674), the smaller ones for prompts, whose rows
+        // see from none to all of the others (1001 tokens of two sequences 35 against 40, 2048 tokens 68 against 72).
         p.tile_rows = s.dim == 128 && (force ? force == 3 : sets(256) >= 256 && 2 * n_new <= s.capacity) ? 256 : 128;
         const int64_t n = prefill_chunks(s, n_new, all, sets(p.tile_rows), tiles);
         chunk = (tiles + n - 1) / n;
     } else {
+        // About three thousand workgroups, of eight tiles at least: shorter chunks spend their time on their beginnings, longer ones leave
+        // compute units without work at the end (32 sequences of up to 256 tiles and 8 heads, 51 us in chunks of 12, 48 of 24, 60 of
+        // 64; 16 of 126 tiles 8.6 of 8, 13.6 of 24).  Short caches are one workgroup's, without a second launch for the sum: 22
+        // tiles in 7.6 us, in chunks 6.0 and 3.9 for the sum.
         p.tile_rows = 16;
         chunk = tiles * sets(16) / 3072;
         if (chunk < 8) chunk = 8;

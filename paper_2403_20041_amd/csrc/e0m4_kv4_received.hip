@@ -5,6 +5,9 @@
 // A workgroup owns 256 rows of the cache, so no two add to one number.  Four pairs of wavefronts hold 64 rows of K each as operands in
 // registers, dequantised once; all rows of queries pass by through LDS, 64 at a time, half of them for either wavefront of a pair.
 // A lane sums what its own query gives to its rows of K; lanes and pairs meet at the end.
+//
+// Bound: arithmetic of the exponentials beside the products, and the first rows of a causal prompt, which all queries see: 2048 tokens,
+// 40 heads in 50 to 55 us.
 #include "e0m4_kv4_attention.h"
 
 namespace e0m4 {
