@@ -386,7 +386,7 @@ int e0m4_int4_gemv(const void* X_f16, const void* codes, int64_t N, int64_t K, i
  *     sequences and `kv_heads` heads, in an opaque layout of e0m4_kv4_bytes()
  *     bytes.  It needs no initialisation.  dim is 64, 128 or 256; group (along
  *     dim) 32, 64 or 128, at most dim; batch and kv_heads <= 65535, capacity <=
- *     2^26, batch * kv_heads * capacity <= 2^40.
+ *     2^26, batch * kv_heads <= 2^24, batch * kv_heads * capacity <= 2^38.
  *   - A row is stored as e0m4_quantize stores a row of weights: per group a
  *     scale and a bias, codes under the same map and rounding.  fp16 and bfloat16
  *     rows alike get fp16 parameters; NaN is stored as 0 and magnitudes above

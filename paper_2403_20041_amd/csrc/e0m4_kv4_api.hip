@@ -8,7 +8,7 @@ namespace e0m4 {
 namespace {
 
 constexpr int64_t kMaxCapacity = (int64_t)1 << 26, kMaxNew = (int64_t)1 << 20, kMaxGrid = 65535, kMaxShare = 1 << 10;
-constexpr int64_t kMaxRows = (int64_t)1 << 40;             // of all sequences and heads
+constexpr int64_t kMaxRows = (int64_t)1 << 38, kMaxSets = (int64_t)1 << 24;   // of all sequences and heads: their workgroups fit a grid
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -17,7 +17,7 @@ int check_kv4(const e0m4_kv4_shape* s)
     if (!s) return E0M4_ERR_NULL;
     if (s->batch < 0 || s->batch > kMaxGrid || s->kv_heads < 0 || s->kv_heads > kMaxGrid || s->capacity < 0 || s->capacity > kMaxCapacity)
         return E0M4_ERR_SHAPE;
-    if (s->batch * s->kv_heads > kMaxRows / (s->capacity ? s->capacity : 1)) return E0M4_ERR_SHAPE;
+    if (s->batch * s->kv_heads > kMaxSets || s->batch * s->kv_heads > kMaxRows / (s->capacity ? s->capacity : 1)) return E0M4_ERR_SHAPE;
     if (s->dim != 64 && s->dim != 128 && s->dim != 256) return E0M4_ERR_SHAPE;
     if ((s->group != 32 && s->group != 64 && s->group != 128) || s->group > s->dim) return E0M4_ERR_GROUP;
     return E0M4_OK;

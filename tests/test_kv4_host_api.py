@@ -140,3 +140,9 @@ def test_python_arguments():
         e0m4.e0m4_kv4_read(cache, shape, zero, 3)
     with pytest.raises(ValueError):
         e0m4.e0m4_kv4_evict(cache, shape, torch.zeros((1, 2, 64)), zero, 8, 2, cache, shape)
+
+
+def test_the_largest_caches(L):
+    size = lambda *s: L.e0m4_kv4_bytes(Shape(*s))  # noqa: E731
+    assert size(4096, 4096, 1, 64, 64) == (1 << 24) * 32 * 72 and size(4097, 4096, 1, 64, 64) == 0
+    assert size(64, 64, 1 << 26, 64, 64) == (1 << 12) * (1 << 21) * 32 * 72 and size(64, 65, 1 << 26, 64, 64) == 0
