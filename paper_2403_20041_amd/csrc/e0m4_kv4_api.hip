@@ -43,18 +43,19 @@ struct Plan {
     size_t out_bytes, stats_bytes, norm_bytes, scores_bytes, queries_bytes;
     size_t bytes() const { return out_bytes + stats_bytes + norm_bytes + scores_bytes + queries_bytes; }
 };
-// Chunks of the cache for many queries.  A workgroup takes about 1.6 us for 64 rows of 128 dims when it is one of few (one head's 16 tokens
-// of 1001, their longest chain 16 times that, 28 us), the device 1.05 us for as many when it is full; partial results go to memory
-// and back, and the launch that adds them takes 4 us at least.
-int64_t prefill_chunks(const e0m4_kv4_shape& s, int64_t n_new, int64_t rows, int64_t sets, int64_t units)
+// Chunks of the cache for many queries.  A workgroup of 128 rows takes 1.45 us for 64 rows of 128 dims alone on a compute unit and 2.1 beside
+// another, one of 256 rows 2.1, the device 1.05 us for 128 rows when it is full.  Partial results go to memory and back and the launch
+// that adds them takes 4 us at least.  32 heads on 2, us in 1, 2, 3, 4, 6 chunks and (and by the estimate): 512 tokens behind 8000 rows
+// 178, 117, 121, 107, 111 (193, 114, 117, 101, 111); 2048 tokens behind 14336 545, 590 and more.
+int64_t prefill_chunks(const e0m4_kv4_shape& s, int64_t n_new, int64_t rows, int64_t sets, int tile_rows, int64_t units)
 {
     const double unit = s.dim / 128.0, seen = n_new < s.capacity ? 1.0 - 0.5 * n_new / s.capacity : 0.5;
-    const double full = sets * units * seen * 1.05 * unit / 256;
+    const double full = sets * (tile_rows / 128) * units * seen * 1.05 * unit / 256;
     double best = 0;
     int64_t chunks = 1;
     for (int64_t c = 1; c <= 64 && c <= units; ++c) {
-        const double chain = (double)((units + c - 1) / c) * 1.6 * unit;
-        const double time = (chain > full ? chain : full) + (c > 1 ? 4.0 + c * (double)rows * s.dim * 8 / 3.5e6 : 0.0);
+        const double chain = (double)((units + c - 1) / c) * (tile_rows == 256 || sets * c > 256 ? 2.1 : 1.45) * unit;
+        const double time = (chain > full ? chain : full) + (c > 1 ? 4.0 + c * (double)rows * s.dim * 8 / 2.6e6 : 0.0);
         if (c == 1 || time < best) {
             best = time;
             chunks = c;
@@ -82,7 +83,7 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
         // they fill the device with like work (2048 tokens behind 14336, 617 us against 674), the smaller ones for prompts, whose rows
         // see from none to all of the others (1001 tokens of two sequences 35 against 40, 2048 tokens 68 against 72).
         p.tile_rows = s.dim == 128 && (force ? force == 3 : sets(256) >= 256 && 2 * n_new <= s.capacity) ? 256 : 128;
-        const int64_t n = prefill_chunks(s, n_new, all, sets(p.tile_rows), tiles);
+        const int64_t n = prefill_chunks(s, n_new, all, sets(p.tile_rows), p.tile_rows, tiles);
         chunk = (tiles + n - 1) / n;
     } else {
         // About three thousand workgroups, of eight tiles at least: shorter chunks spend their time on their beginnings, longer ones leave
