@@ -8,8 +8,8 @@
 // + i of a tile of 32, slot 4 (a & 1) + i of octet 2 (a >> 1) + kh.
 //
 // Bound: 32 products of 32 cycles and about 330 cycles of other instructions (four each, exponentials sixteen) per wavefront and 64
-// rows share a SIMD between two wavefronts; under the clock of a full load 32 heads on 2, 2048 tokens behind 14336 rows take 501 to 583
-// us, 883 to 1028 TFLOP/s (a large library product: 1147).  Prompts are bound by the rows that see most: 64 rows of the cache
+// rows share a SIMD between two wavefronts; under the clock of a full load 32 heads on 2, 2048 tokens behind 14336 rows take 501 to 551
+// us, 935 to 1028 TFLOP/s (a large library product: 1147).  Prompts are bound by the rows that see most: 64 rows of the cache
 // follow each other every 1.4 us there.
 #include "e0m4_kv4_attention.h"
 
