@@ -434,8 +434,9 @@ int e0m4_kv4_read(const void* cache, const e0m4_kv4_shape* shape, const int32_t*
  * the sum of row j's softmax weights over the queries and the heads of g, for j <
  * lengths[b] (what lies behind is not touched).
  * Scores, sums and products are accumulated in fp32, the softmax weights are
- * rounded to fp16 for their product with the values; bfloat16 queries are used as
- * fp16 after scaling each by a power of two.  Workspace as for e0m4_matmul
+ * rounded to fp16 for their product with the values (with few fp16 queries what
+ * that leaves is multiplied too); bfloat16 queries are used as fp16 after scaling
+ * each by a power of two.  Workspace as for e0m4_matmul
  * (e0m4_kv4_attention_workspace_bytes bytes).  The result is deterministic.
  */
 size_t e0m4_kv4_attention_workspace_bytes(const e0m4_kv4_shape* shape, int64_t heads, int64_t n_new, int with_weights);
