@@ -45,12 +45,15 @@ class Kv4AttentionBlock:
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         """x [batch, n, hidden] fp16, the next n tokens of every sequence -> the block's output, of the same shape."""
         batch, n, hidden = x.shape
-        if self.most + n > self.shape.capacity:
-            self.evict()
-            if self.most + n > self.shape.capacity:
-                raise ValueError("%d tokens do not fit behind the %d rows that stay" % (n, self.most))
+        if batch != self.shape.batch or hidden != self.hidden:
+            raise ValueError("x must be [%d, n, %d], got %s" % (self.shape.batch, self.hidden, tuple(x.shape)))
+        # (all that can refuse the call comes before the eviction: rows that left are gone)
+        if min(self.most, self.budget) + n > self.shape.capacity:
+            raise ValueError("%d tokens do not fit behind the %d rows that stay" % (n, min(self.most, self.budget)))
         flat = x.reshape(batch * n, hidden)
         qkv = e0m4.e0m4_matmul_fused(flat, self.qkv, self.columns, hidden, self.group, rms_gamma=self.gamma, rms_eps=1e-5)
+        if self.most + n > self.shape.capacity:
+            self.evict()
         q, k, v = (t.view(batch, n, -1, self.dim) for t in qkv.view(batch, n, -1).split(
             (hidden, self.kv_heads * self.dim, self.kv_heads * self.dim), dim=-1))
         e0m4.e0m4_kv4_append(self.cache, self.shape, k, v, self.lengths)
