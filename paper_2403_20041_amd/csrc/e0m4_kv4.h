@@ -149,6 +149,17 @@ struct Kv4Attention {
     float* scores;                                      // [batch][kv_heads][rows][tiles * 32] in powers of two, or null
 };
 
+// Grid of one workgroup for each sequence, head and one of `places`, place by place: x counts heads, y sequences and z places; places
+// that z has no room for (65535) go to x in runs, the last of which may count beyond `places`.  A launch may have less than 2^32
+// work items along a dimension: heads are at most 65535 and heads times places 2^36 (2^30 blocks of the cache; 2^25 blocks of queries
+// in up to 2^11 chunks), so that x is at most 2^21 workgroups.
+inline dim3 kv4_place_grid(const Kv4Attention& a, int64_t places)
+{
+    const int64_t run = (places + 65534) / 65535;
+    return dim3((unsigned)(a.kv_heads * run), (unsigned)a.batch, (unsigned)((places + run - 1) / run));
+}
+__device__ inline int kv4_place(const Kv4Attention& a) { return blockIdx.z * (gridDim.x / a.kv_heads) + blockIdx.x / a.kv_heads; }
+
 __device__ inline int kv4_query_of(const Kv4Attention& a, int row) { return a.share_inverse ? (int)__umulhi((uint32_t)row, a.share_inverse) : row; }
 
 // What a tile of `n` rows of queries, the first one `row0`, looks at.

@@ -120,12 +120,12 @@ int check_attention(const e0m4_kv4_shape* s, int64_t heads, int64_t n_new)
 
 __global__ void kv4_zero_kernel(uint4* y, int64_t pieces)
 {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < pieces) y[i] = uint4{0, 0, 0, 0};
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * blockDim.x) y[i] = uint4{0, 0, 0, 0};
 }
 int zero_fill(void* y, int64_t bytes, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv4_zero_kernel, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, stream, static_cast<uint4*>(y), bytes / 16);
+    const int64_t blocks = (bytes / 16 + 255) / 256;    // (a launch of 2^32 work items is refused)
+    hipLaunchKernelGGL(kv4_zero_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream, static_cast<uint4*>(y), bytes / 16);
     return check_launch();
 }
 

@@ -385,6 +385,9 @@ int launch_kv4_decode(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_
 {
     const int64_t rows = (int64_t)a.n_new * a.share, row_tiles = (rows + kCols - 1) / kCols;
     const int cols = rows < kCols ? (int)rows : kCols;
+    // 2^32 work items along a dimension are refused by the launch itself; only a forced kernel or chunk comes near: by choice these are at
+    // most 12000 tiles of rows and chunks
+    if (row_tiles * a.chunks * 512 > 0xffffffffLL) return E0M4_ERR_SHAPE;
     const dim3 grid((unsigned)(row_tiles * a.chunks), (unsigned)a.kv_heads, (unsigned)a.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;

@@ -45,9 +45,9 @@ __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 1 : 2) void kv4_prefill_ke
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, kh = lane >> 5;
     const int rows = a.n_new * a.share;
     // of all sequences and heads the rows that see most first
-    const unsigned per_block = (unsigned)a.kv_heads * a.batch, place = blockIdx.x / per_block;
-    const int h = blockIdx.x % per_block % a.kv_heads, b = blockIdx.x % per_block / a.kv_heads, chunk = place % a.chunks;
-    const int block_row = (int)((rows + kRows - 1) / kRows - 1 - place / a.chunks) * kRows;
+    const int h = blockIdx.x % a.kv_heads, b = blockIdx.y, place = kv4_place(a), chunk = place % a.chunks;
+    const int block_row = ((rows + kRows - 1) / kRows - 1 - place / a.chunks) * kRows;
+    if (block_row < 0) return;
     const int block_rows = rows - block_row < kRows ? rows - block_row : kRows;
     const Kv4Span span = kv4_span(a, b, block_row, block_rows);
     const int unit0 = span.begin / kKeys + chunk * a.chunk_tiles, units_end = (span.end + kKeys - 1) / kKeys;
@@ -287,8 +287,7 @@ int launch_prefill(const Kv4Attention& a, dim3 grid, hipStream_t stream)
 int launch_kv4_prefill(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.n_new * a.share, blocks = (rows + a.tile_rows - 1) / a.tile_rows;
-    if (blocks * a.chunks * a.kv_heads * a.batch > 0x7fffffffLL) return E0M4_ERR_SHAPE;
-    const dim3 grid((unsigned)(blocks * a.chunks * a.kv_heads * a.batch));
+    const dim3 grid = kv4_place_grid(a, blocks * a.chunks);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
         if constexpr (DIM == 128)

@@ -26,8 +26,7 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, kh = lane >> 5;
     const int set = wave & 3, half = wave >> 2, rows = a.n_new * a.share;
     // rows of the cache that most queries see first
-    const unsigned per_block = (unsigned)a.kv_heads * a.batch;
-    const int h = blockIdx.x % per_block % a.kv_heads, b = blockIdx.x % per_block / a.kv_heads, key0 = blockIdx.x / per_block * kKeys;
+    const int h = blockIdx.x % a.kv_heads, b = blockIdx.y, key0 = kv4_place(a) * kKeys;
     const int length = clamp_count(a.lengths[b], a.capacity), count = a.counts ? clamp_count(a.counts[b], a.n_new) : a.n_new;
     if (key0 >= length || count == 0) return;
     const int64_t bh = (int64_t)b * a.kv_heads + h;
@@ -171,11 +170,10 @@ __global__ __launch_bounds__(kThreads) void kv4_received_kernel(Kv4Attention a, 
 
 int launch_kv4_received(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream)
 {
-    const int64_t blocks = (s.capacity + kKeys - 1) / kKeys * s.kv_heads * s.batch;
-    if (blocks > 0x7fffffffLL) return E0M4_ERR_SHAPE;
+    const dim3 grid = kv4_place_grid(a, (s.capacity + kKeys - 1) / kKeys);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
-        hipLaunchKernelGGL((kv4_received_kernel<DIM, G>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, received);
+        hipLaunchKernelGGL((kv4_received_kernel<DIM, G>), grid, dim3(kThreads), 0, stream, a, received);
         return check_launch();
     });
 }
