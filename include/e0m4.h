@@ -453,7 +453,9 @@ int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, i
  * batch, heads, dim and group with capacity >= budget >= 1.
  *   received is [batch, kv_heads, capacity] fp32.  kept [batch, kv_heads, budget]
  * int32 gets their row numbers, received_out (same shape, fp32) what they received
- * (-1 and 0 behind the last), lengths_out [batch] min(lengths[b], budget).
+ * (-1 and 0 behind the last), lengths_out [batch] min(lengths[b], budget);
+ * lengths_out may be lengths, nothing else that is written may overlap what is
+ * read.
  */
 int e0m4_kv4_evict(const void* cache, const e0m4_kv4_shape* shape, const float* received, const int32_t* lengths,
                    int64_t budget, int64_t recent, void* small, const e0m4_kv4_shape* small_shape, int32_t* kept,

@@ -291,8 +291,7 @@ __device__ inline float weight_of_rank(uint32_t r) { return __builtin_bit_cast(f
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kHeld = 28672;
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float* __restrict__ received, int64_t capacity, int held_most,
                                                                     const int* __restrict__ lengths, int budget, int recent,
-                                                                    int* __restrict__ kept, int* __restrict__ lengths_out,
-                                                                    float* __restrict__ received_out)
+                                                                    int* __restrict__ kept, float* __restrict__ received_out)
 {
     static_assert(kBins == 2 * kSelectThreads && kCopies == 4, "two counters of four copies per thread");
     extern __shared__ uint32_t held[];
@@ -305,7 +304,6 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
     int* k = kept + bh * budget;
     float* ro = received_out + bh * budget;
     const int n = clamp_count(lengths[b], capacity);
-    if (t == 0 && h == 0) lengths_out[b] = n < budget ? n : budget;
     if (n <= budget) {
         for (int i = t; i < budget; i += kSelectThreads) {
             k[i] = i < n ? i : -1;
@@ -428,17 +426,23 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
     newest();
 }
 
-// The rows that stay move to the smaller cache as they are.  One workgroup per tile of it: words of K are copied, words of V put
+// The rows that stay move to the smaller cache as they are, and the number of them becomes the sequence's length: here, because the
+// selection's workgroups of all heads read the old one, which may stand in the same place.  One workgroup per tile of it: words of K are copied, words of V put
 // together from the eight rows' words, which takes nearly all of the old cache from memory: 46000 rows of 40 heads to 16384 in 91
 // us, 265 MB read and 94 written.
 template <int DIM, int G>
 __global__ __launch_bounds__(DIM) void kv4_gather_kernel(const uint8_t* __restrict__ cache, int64_t tiles, const int* __restrict__ kept,
-                                                              int budget, uint8_t* __restrict__ small, int64_t small_tiles)
+                                                              int budget, uint8_t* __restrict__ small, int64_t small_tiles, int64_t capacity,
+                                                              const int* lengths, int* lengths_out)
 {
     using L = Kv4<DIM, G>;
     __shared__ int rows[kKv4Rows];
     const int b = blockIdx.z, h = blockIdx.y, t = threadIdx.x;
     const int64_t bh = (int64_t)b * gridDim.y + h;
+    if (blockIdx.x == 0 && h == 0 && t == 0) {
+        const int n = clamp_count(lengths[b], capacity);
+        lengths_out[b] = n < budget ? n : budget;
+    }
     if (t < kKv4Rows) {
         const int64_t i = (int64_t)blockIdx.x * kKv4Rows + t;
         rows[t] = i < budget ? kept[bh * budget + i] : -1;
@@ -536,14 +540,14 @@ int launch_kv4_evict(const void* cache, const e0m4_kv4_shape& s, const float* re
     if (rc != E0M4_OK) return rc;
     const int held = s.capacity < kHeld ? (int)s.capacity : kHeld;
     hipLaunchKernelGGL(kv4_select_kernel, dim3((unsigned)s.kv_heads, (unsigned)s.batch), dim3(kSelectThreads), held * 4, stream, received,
-                       s.capacity, held, lengths, budget, recent, kept, lengths_out, received_out);
+                       s.capacity, held, lengths, budget, recent, kept, received_out);
     rc = check_launch();
     if (rc != E0M4_OK) return rc;
     const dim3 grid((unsigned)kv4_tiles(budget), (unsigned)s.kv_heads, (unsigned)s.batch);
     return kv4_dispatch(s, [&](auto shape) -> int {
         constexpr int DIM = decltype(shape)::kDim, G = decltype(shape)::kGroup;
         hipLaunchKernelGGL((kv4_gather_kernel<DIM, G>), grid, dim3(DIM), 0, stream, static_cast<const uint8_t*>(cache),
-                           kv4_tiles(s.capacity), kept, budget, static_cast<uint8_t*>(small), kv4_tiles(o.capacity));
+                           kv4_tiles(s.capacity), kept, budget, static_cast<uint8_t*>(small), kv4_tiles(o.capacity), s.capacity, lengths, lengths_out);
         return check_launch();
     });
 }
