@@ -319,6 +319,10 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(Kv4Attenti
         float* factor = factors[wave];
         float top;
         const float total = chunk_factors(a.part_stats + at, stride, chunks, lane, top, factor);
+        // the other lanes' factors: a wavefront's LDS accesses stay in their order, if only the compiler keeps it
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         const int d = lane % kPer * 4;
         const float* p = a.part_out + at * DIM + d;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
