@@ -423,21 +423,26 @@ int e0m4_kv4_read(const void* cache, const e0m4_kv4_shape* shape, const int32_t*
 
 /*
  * Attention of queries [batch, n_new, heads, dim], the newest counts[b] of the
- * lengths[b] rows of each sequence (already appended), over the cache:
+ * lengths[b] rows of each sequence (all of them appended, also those that a mask
+ * or a window hides), over the cache:
  *     out[b,i,h] = sum_j softmax_j(q[b,i,h] . k[b,j,g] / sqrt(dim)) v[b,j,g],
  * g = h / (heads / kv_heads), over the rows j that query i sees: j < lengths[b];
  * if `causal`, j <= p = lengths[b] - counts[b] + i; if window > 0 (causal only), j >
- * p - window; if `mask`, those it has set.  A query that sees no row, and queries
- * i >= counts[b], get zeros.  out is [batch, n_new, heads, dim] in the queries'
- * type.  heads / kv_heads <= 1024, n_new <= 2^20, heads / kv_heads * n_new <= 2^22.
+ * p - window; if `mask`, those it has set.  Places are those of rows in the cache:
+ * after an eviction a window counts the rows that stayed, not tokens.  A query that
+ * sees no row, and queries i >= counts[b], get zeros.  out is [batch, n_new, heads,
+ * dim] in the queries' type.  heads / kv_heads <= 1024, n_new <= 2^20, heads / kv_heads * n_new <= 2^22,
+ * batch * heads * n_new <= 2^32.
  *   weights (NULL: none) is [batch, kv_heads, capacity] fp32; weights[b,g,j] +=
  * the sum of row j's softmax weights over the queries and the heads of g, for j <
  * lengths[b] (what lies behind is not touched).
  * Scores, sums and products are accumulated in fp32, the softmax weights are
  * rounded to fp16 for their product with the values (with few fp16 queries what
  * that leaves is multiplied too); bfloat16 queries are used as fp16 after scaling
- * each by a power of two.  Workspace as for e0m4_matmul
- * (e0m4_kv4_attention_workspace_bytes bytes).  The result is deterministic.
+ * each by a power of two.  Scores q . k / sqrt(dim) are taken to be below 2^23 in
+ * magnitude; beyond that fp32 has no digits for their differences, and outputs mean
+ * nothing.  Workspace as for e0m4_matmul (e0m4_kv4_attention_workspace_bytes bytes).
+ * The result is deterministic.
  */
 size_t e0m4_kv4_attention_workspace_bytes(const e0m4_kv4_shape* shape, int64_t heads, int64_t n_new, int with_weights);
 int e0m4_kv4_attention(const e0m4_kv4_rows* queries, int dtype, int64_t heads, int64_t n_new, const void* cache,

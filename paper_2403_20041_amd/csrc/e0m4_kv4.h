@@ -222,7 +222,7 @@ int launch_kv4_prefill(const Kv4Attention& a, const e0m4_kv4_shape& s, hipStream
 constexpr int kKv4MaxChunks = 2048;
 // (received, unless null: the rows' weights from the scores, in the same launch)
 int launch_kv4_combine(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream);
-// received[j] += the weights of row j, from the rows' log2 sums
+// received[j] += the weights of row j, from the rows' references and factors (norm)
 int launch_kv4_received(const Kv4Attention& a, const e0m4_kv4_shape& s, float* received, hipStream_t stream);
 
 }  // namespace e0m4

@@ -4,7 +4,9 @@
 
 rms-norm and the qkv projection are one e0m4_matmul_fused call, whose output's columns the append reads as they are; the output
 projection adds the residual.  The attention collects what every cached row receives; when the cache is full, the rows that received
-least leave it (e0m4_kv4_evict) and the tokens go on from there.
+least leave it (e0m4_kv4_evict) and the tokens go on from there.  There is no rotary embedding here: a model that has one turns
+queries and keys between the projection and the append, by the number of tokens that came before and not by the rows in the cache,
+which are fewer after an eviction; rows in the cache keep the angle of their own token.
 """
 from __future__ import annotations
 
