@@ -45,8 +45,8 @@ struct Plan {
 };
 // Chunks of the cache for many queries.  A workgroup of 128 rows takes 1.45 us for 64 rows of 128 dims alone on a compute unit and 2.1 beside
 // another, one of 256 rows 2.1, the device 1.05 us for 128 rows when it is full.  Partial results go to memory and back and the launch
-// that adds them takes 4 us at least.  32 heads on 2, us in 1, 2, 3, 4, 6 chunks and (and by the estimate): 512 tokens behind 8000 rows
-// 178, 117, 121, 107, 111 (193, 114, 117, 101, 111); 2048 tokens behind 14336 545, 590 and more.
+// that adds them takes 4 us at least.  32 heads on 2, us in 1, 2, 3, 4, 6 chunks (and by the estimate): 512 tokens behind 8000 rows
+// 180, 113, 114, 102, 108 (193, 114, 117, 101, 111); 2048 tokens behind 14336 508, 561, 565, 586, 603.
 int64_t prefill_chunks(const e0m4_kv4_shape& s, int64_t n_new, int64_t rows, int64_t sets, int tile_rows, int64_t units)
 {
     const double unit = s.dim / 128.0, seen = n_new < s.capacity ? 1.0 - 0.5 * n_new / s.capacity : 0.5;
@@ -63,15 +63,20 @@ int64_t prefill_chunks(const e0m4_kv4_shape& s, int64_t n_new, int64_t rows, int
     }
     return chunks;
 }
+// Everything here goes by the capacity, for the lengths are on the device: in caches much larger than their sequences, and under short
+// windows, chunks are longer than the rows that there are would have them.  32 sequences of up to 8192 rows, 32 heads on 8, 47 us at
+// that capacity, 62 and 95 at 4 and 16 times it; one of 701 rows 8.5, 11.8, 11.9; prompts 34, 33, 32.
 Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool weights)
 {
     Plan p;
     const int64_t rows = heads / s.kv_heads * n_new, all = s.batch * s.kv_heads * rows;
     const int force = knob(Knob::kv4_attention);
     // The kernel for few queries dequantises the cache again for every 16 rows of them, the other one shares it among 128, but has longer
-    // chains and leaves a workgroup's missing rows idle.  8 sequences of 3000 rows and 8 heads, us of the two: 49 rows of queries 31
-    // and 29, 97 rows 42 and 38, 33 rows 24 and 27; 500 rows, 129 rows of queries 14 and 21; 16 sequences of 500 rows and 8 heads, 193
-    // rows of queries (36608 tiles taken) 22 and 18, one of 16000 and 2 heads (13026) 29 and 25, of 3000 (2470) 15 and 18.
+    // chains and leaves a workgroup's missing rows idle.  8 sequences of 3000 rows and 8 heads, us of the two: 65 rows of queries 44
+    // and 32, 97 rows 50 and 33; 8 of 500 rows and 8 heads, 129 rows of queries (9216 tiles taken) 16 and 18, 16 of them, 193 rows
+    // (26624) 31 and 18; one of 16000 and 2 heads, 208 rows (13000) 26 and 23, of 3000 (2444) 13 and 15.  Up to 64 rows are the first
+    // one's, which multiplies whole weights for fp16 results, though the other is the faster from about 33 on (31 and 26 us, 49 rows
+    // 34 and 28).
     const int64_t taken = (s.capacity + kKv4Rows - 1) / kKv4Rows * s.batch * s.kv_heads * ((rows + 15) / 16);
     p.prefill = force ? force >= 2 : rows > 64 && taken > 12000;
     p.tile_keys = p.prefill ? kKv4PrefillKeys : kKv4Rows;
@@ -80,16 +85,16 @@ Plan plan_attention(const e0m4_kv4_shape& s, int64_t heads, int64_t n_new, bool 
     int64_t chunk;
     if (p.prefill) {
         // 256 rows to a workgroup halve the dequantisation of 128, two workgroups of which a compute unit has at once: the larger ones where
-        // they fill the device with like work (2048 tokens behind 14336, 617 us against 674), the smaller ones for prompts, whose rows
-        // see from none to all of the others (1001 tokens of two sequences 35 against 40, 2048 tokens 68 against 72).
+        // they fill the device with like work (2048 tokens behind 14336, 508 us against 553), the smaller ones for prompts, whose rows
+        // see from none to all of the others (1001 tokens of two sequences 33 against 37, 2048 tokens 55 against 62).
         p.tile_rows = s.dim == 128 && (force ? force == 3 : sets(256) >= 256 && 2 * n_new <= s.capacity) ? 256 : 128;
         const int64_t n = prefill_chunks(s, n_new, all, sets(p.tile_rows), p.tile_rows, tiles);
         chunk = (tiles + n - 1) / n;
     } else {
         // About three thousand workgroups, of eight tiles at least: shorter chunks spend their time on their beginnings, longer ones leave
-        // compute units without work at the end (32 sequences of up to 256 tiles and 8 heads, 51 us in chunks of 12, 48 of 24, 60 of
-        // 64; 16 of 126 tiles 8.6 of 8, 13.6 of 24).  Short caches are one workgroup's, without a second launch for the sum: 22
-        // tiles in 7.6 us, in chunks 6.0 and 3.9 for the sum.
+        // compute units without work at the end (32 sequences of up to 256 tiles and 8 heads, 50 us in chunks of 8, 44 of 24, 50 of
+        // 64; 16 of up to 126 tiles and a head of 256 dims 16.0 of 4, 15.2 of 8, 18.2 of 24).  Short caches are one workgroup's,
+        // without a second launch for the sum: 22 tiles in 9.8 us, 14.3 in chunks.
         p.tile_rows = 16;
         chunk = tiles * sets(16) / 3072;
         if (chunk < 8) chunk = 8;

@@ -101,7 +101,8 @@ __device__ inline uint32_t word_of_pairs(uint32_t p0, uint32_t p1, uint32_t p2, 
 // One workgroup per tile of the cache that the new rows touch.  A row is DIM / 8 neighbouring threads with 8 values each; a group is
 // G / 8 lanes, its range is found among them.  A thread's eight K codes are one word of the layout.  V codes go through LDS, 16 bits
 // each, because a word of V holds eight rows; a word that also holds rows which stay is read and merged.  Two prompts of 2048 and 1536
-// tokens, 40 heads: 27 us for 81 MB, about a hundred instructions for eight values; one token of a sequence 3.4 us.
+// tokens, 40 heads: 27 us for 94 MB, which a copy moves in 18; about a hundred instructions for eight values take 12, and a workgroup
+// does one after the other.  One token of a sequence 3.4 us.
 template <int DIM, int G, bool BF16>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restrict__ cache, int64_t capacity, int64_t tiles, Kv4Rows keys,
                                                               Kv4Rows values, int64_t n_new, const int* __restrict__ starts,
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(uint8_t* __restric
 }
 
 // One workgroup per tile of the cache that the rows first ... first + rows - 1 touch: the codes' values go to LDS, whence rows are
-// written out in whole.  Rows outside [0, min(length, capacity)) read as zeros.  Bound by memory: those two prompts in 17 us, 4.7 TB/s.
+// written out in whole.  Rows outside [0, min(length, capacity)) read as zeros.  Bound by memory: those two prompts in 17.5 us, 5.4 TB/s.
 template <int DIM, int G>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(const uint8_t* __restrict__ cache, int64_t capacity, int64_t tiles,
                                                             const int* __restrict__ lengths, const int* __restrict__ firsts, int64_t rows,
@@ -286,8 +287,9 @@ __device__ inline float weight_of_rank(uint32_t r) { return __builtin_bit_cast(f
 // over its bits from the top, then one pass that counts and one that writes the rows above it, and the first ones that equal it, in
 // order; a wavefront has a contiguous part of the rows in both, so that places come from ballots and sixteen sums.  A counter is
 // four, one for every fourth lane: weights share their upper bits, and additions to one address follow each other.  After the
-// first pass the ranks of the first kHeld rows are in LDS.  What bounds it is arithmetic: one compute unit has a head's rows (16000 of
-// them in 21 us, 8000 in 13).
+// first pass the ranks of the first kHeld rows are in LDS.  One compute unit has a head's rows (16000 of them in 18 to 22 us, 8000 in 13);
+// what bounds it there are the additions in LDS, the barriers between the passes and the last one, which goes from 64 rows to the
+// next.
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kHeld = 28672;
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float* __restrict__ received, int64_t capacity, int held_most,
                                                                     const int* __restrict__ lengths, int budget, int recent,
@@ -427,9 +429,9 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(const float*
 }
 
 // The rows that stay move to the smaller cache as they are, and the number of them becomes the sequence's length: here, because the
-// selection's workgroups of all heads read the old one, which may stand in the same place.  One workgroup per tile of it: words of K are copied, words of V put
-// together from the eight rows' words, which takes nearly all of the old cache from memory: 46000 rows of 40 heads to 16384 in 91
-// us, 265 MB read and 94 written.
+// selection's workgroups of all heads read the old one, which may stand in the same place.  One workgroup per tile of the smaller cache:
+// words of K are copied, words of V put together from the eight rows' words, which takes nearly all of the old cache from memory: 46000
+// rows of 40 heads to 16384 in 91 us, 265 MB read and 94 written, 3.9 TB/s.
 template <int DIM, int G>
 __global__ __launch_bounds__(DIM) void kv4_gather_kernel(const uint8_t* __restrict__ cache, int64_t tiles, const int* __restrict__ kept,
                                                               int budget, uint8_t* __restrict__ small, int64_t small_tiles, int64_t capacity,

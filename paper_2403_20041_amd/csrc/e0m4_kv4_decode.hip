@@ -105,14 +105,16 @@ __device__ inline uint32_t seen_rows(const Kv4Attention& a, int b, int row0, int
 
 // What the rounding of P to fp16 leaves is multiplied too where the result is fp16, whose own rounding is no larger than that of the few
 // weights that make a short row: by a second product (kRestSecond), or, where there are at most eight rows of queries, in the upper
-// eight columns of the one that there is, which hold the same rows again (kRestColumns: 32 heads on 8, 32 sequences of up to 8192 rows,
-// 51 us; with a second product 56, with neither 50).
+// eight columns of the one that there is, which hold the same rows again (kRestColumns).  32 heads on 8, 32 sequences of up to 8192
+// rows: 44.0 us in columns, 44.6 with a second product, 41.8 with neither; 64 sequences of 4000 rows of 64 dims 34.8, 35.7, 32.2; 16 of
+// 8000 rows of 256 dims 85.6, 83.9, 81.7.
 enum Rest { kRestNone, kRestSecond, kRestColumns };
 
-// Bound: a tile of 32 rows is 4352 bytes (dim 128, group 128) and about 300 vector instructions, 208 of them dequantisation, so that
-// memory (4.2 TB/s is the most that this kernel has drawn) and arithmetic take about as long; four wavefronts a SIMD with a tile each on its
-// way cover the latency, two tiles ahead gained nothing (49 against 48 us).  32 sequences of up to 8192 rows, 32 heads on 8: 182 MB in 48
-// us; 4 of up to 16000 rows, 40 heads, with their scores kept: 272 MB in 66 us.
+// Bound: a tile of 32 rows is 4352 bytes (dim 128, group 128) and about 300 vector instructions, 208 of them dequantisation.  32 sequences
+// of up to 8192 rows, 32 heads on 8: 182 MB in 48 us, of which a copy would take 35, the instructions 20 and the products 4: memory, and
+// what of the rest does not fall behind its loads.  Four wavefronts a SIMD have a tile each on its way; two tiles ahead gained
+// nothing (49 against 48 us).  4 of up to 16000 rows, 40 heads, with their scores kept: 272 MB in 67 us.  4.2 TB/s is the most that
+// this kernel has drawn.
 template <int DIM, int G, int WAVES, Rest REST>
 __global__ __launch_bounds__(WAVES * 64, DIM == 256 ? 2 : DIM == 128 && G == 32 ? 3 : 4) void kv4_decode_kernel(Kv4Attention a)
 {

@@ -8,9 +8,13 @@
 // + i of a tile of 32, slot 4 (a & 1) + i of octet 2 (a >> 1) + kh.
 //
 // Bound: 32 products of 32 cycles and about 330 cycles of other instructions (four each, exponentials sixteen) per wavefront and 64
-// rows share a SIMD between two wavefronts; under the clock of a full load 32 heads on 2, 2048 tokens behind 14336 rows take 501 to 551
-// us, 935 to 1028 TFLOP/s (a large library product: 1147).  Prompts are bound by the rows that see most: 64 rows of the cache
-// follow each other every 1.4 us there.
+// rows share a SIMD between two wavefronts; 32 heads on 2, 2048 tokens behind 14336 rows take 513 us, 1004 TFLOP/s (a large library product:
+// 1147), once some tens of passes have settled the clock, and 590 to 630 in the first ones.  Prompts are bound by the rows that see
+// most: 64 rows of the cache follow each other every 1.4 to 2.1 us there.
+//
+// What the rounding of P to fp16 leaves is not multiplied here.  With a second product for it those 513 us are 720 and two prompts of
+// 1001 tokens 46 instead of 37, for an error of fp16 results against 64 bits of 2.1e-4 (their own rounding) instead of 2.7e-4;
+// bfloat16 results do not change (1.67e-3).
 #include "e0m4_kv4_attention.h"
 
 namespace e0m4 {

@@ -7,7 +7,7 @@
 // A lane sums what its own query gives to its rows of K; lanes and pairs meet at the end.
 //
 // Bound: arithmetic of the exponentials beside the products, and the first rows of a causal prompt, which all queries see: 2048 tokens,
-// 40 heads in 50 to 55 us.
+// 40 heads in 49 to 53 us.
 #include "e0m4_kv4_attention.h"
 
 namespace e0m4 {
