@@ -11,8 +11,6 @@ import pytest
 
 from paper_2403_20041_amd import binding, build
 
-ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-
 RECORDER = r"""
 #include <cstddef>
 #include <cstdio>
@@ -41,6 +39,7 @@ class Shape(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("capacity", ctypes.c_int64), ("dim", ctypes.c_int), ("group", ctypes.c_int)]
 class Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("batch_ld", ctypes.c_int64), ("row_ld", ctypes.c_int64), ("head_ld", ctypes.c_int64)]
+ctypes.CDLL(sys.argv[2], mode=ctypes.RTLD_GLOBAL)     # its definitions come before those of the library's own dependencies
 L = ctypes.CDLL(sys.argv[1])
 P, FAR, i64, vp, sz = ctypes.c_void_p(0x1000), ctypes.c_void_p(1 << 50), ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
 rows = ctypes.byref(Rows(0x1000, 0, 0, 0))
@@ -78,9 +77,7 @@ def run(tmp_path_factory):
     subprocess.run([compiler, "-shared", "-fPIC", "-O1", "-o", library, str(folder / "recorder.cpp")], check=True)
 
     def go(calls):
-        before = os.environ.get("LD_PRELOAD")
-        env = dict(os.environ, LD_PRELOAD=library + (":" + before if before else ""))
-        text = subprocess.run([sys.executable, str(folder / "caller.py"), binding.LIB_PATH], input=json.dumps(calls), env=env, check=True, timeout=120,
+        text = subprocess.run([sys.executable, str(folder / "caller.py"), binding.LIB_PATH, library], input=json.dumps(calls), check=True, timeout=120,
                               stdout=subprocess.PIPE, universal_newlines=True).stdout
         out, launches = [], []
         for line in text.splitlines():
