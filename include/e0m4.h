@@ -467,6 +467,94 @@ int e0m4_kv4_evict(const void* cache, const e0m4_kv4_shape* shape, const float* 
                    int32_t* lengths_out, float* received_out, void* stream);
 
 /*
+ * Rows that choose their weights: a token of a mixture of experts goes through some
+ * of the experts' feed-forward weights, a row of a batch that many users share
+ * through the low-rank adapter of its user.  e0m4_route chooses a token's experts
+ * and e0m4_groups lays entries out by what they chose; the products, the sum of a
+ * token's rows and the adapters read that layout.
+ *   - A layout is for `rows` entries and `groups` weights to choose from: rows <=
+ *     2^24, 1 <= groups <= 1023.  Its memory, e0m4_groups_bytes() bytes, 16-byte
+ *     aligned, begins with int32 arrays, each padded to a multiple of four elements:
+ *       offsets [groups + 1]  where each group begins; offsets[groups] entries in all
+ *       order [rows]          the entries, group after group, each group's in
+ *                             ascending order, then those of no group, ascending
+ *       place [rows]          where each entry is in `order`, -1 for those of no group
+ *     and goes on with what the library keeps for itself.  It is read by calls that
+ *     name the same rows and groups, and free for reuse once these have completed.
+ * Errors, streams and empty problems are as elsewhere in this file, results are
+ * deterministic.
+ */
+#define E0M4_FP16 0
+#define E0M4_BF16 1
+#define E0M4_FP32 2
+
+size_t e0m4_groups_bytes(int64_t rows, int64_t groups);
+
+/* The layout of entries i < rows by index[i] (device memory); values outside [0, groups) are of no group. */
+int e0m4_groups(const int32_t* index, int64_t rows, int64_t groups, void* plan, void* stream);
+
+/*
+ * Router: of the logits [tokens, experts] (rows logits_ld elements apart) each token's
+ * k largest, k <= 16 and experts <= 1023, largest first, ties to the lower expert, and their weights
+ *   E0M4_ROUTE_SOFTMAX  exp(l) / the sum of exp over all experts,
+ *   E0M4_ROUTE_SIGMOID  1 / (1 + exp(-l)),
+ * with `renormalise` divided by their sum over the k chosen ones, times factor; fp32.
+ * Infinite logits count as the largest finite ones, NaN as the lowest.  Tokens from
+ * count[0] on (device memory; NULL: none), as in a batch that is padded to a fixed size, choose no expert:
+ * chosen -1, weights 0.  chosen and weights are [tokens, k].  `plan` (NULL: none)
+ * gets the layout of the tokens * k entries by expert; entry t * k + j is token t's j-th.
+ */
+#define E0M4_ROUTE_SOFTMAX 0
+#define E0M4_ROUTE_SIGMOID 1
+int e0m4_route(const void* logits, int dtype, int64_t tokens, int64_t experts, int64_t logits_ld, int k, int scoring, int renormalise, float factor,
+               const int32_t* count, int32_t* chosen, float* weights, void* plan, void* stream);
+
+/*
+ * Products grouped by weights: for p < offsets[groups], with e = order[p] and g its group,
+ *     a[p, n] = sum_k X[r, k] * dequant(codes of g)[n, k],
+ * r = e / share (a token's row for each of its `share` entries; rows % share == 0), or
+ * r = p with share = 0 (rows that lie in the layout's order, as these calls write them);
+ * E0M4_EPILOGUE_SWIGLU: Y = silu(gate) * up of the two halves of n, as in
+ * e0m4_matmul_fused (N a multiple of 64).  Y is [rows, N] (or N / 2); its rows from
+ * offsets[groups] on are left as they were.  `codes` holds the packed buffers of the
+ * groups' weights [N, K] one after the other, each of e0m4_codes_bytes(N, K, group)
+ * (e0m8_codes_bytes) bytes.  N <= 2^24, 0 < K, K as for e0m4_matmul (e0m8_matmul), with
+ * share > 0 X of less than 2 GiB, gated the gate's half of a buffer of at most 1 GiB.
+ * Accumulation is fp32; tiles of many rows, and groups of 32 and 64, multiply weights
+ * rounded as e0m4_dequant rounds them, the others the codes' exact values.  Y may not
+ * overlap X.  No workspace.
+ */
+int e0m4_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
+                        int group, int epilogue, void* Y_f16, void* stream);
+int e0m8_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
+                        int group, int epilogue, void* Y_f16, void* stream);
+int e0m4_bf16_matmul_grouped(const void* X_bf16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
+                             int group, int epilogue, void* Y_bf16, void* stream);
+
+/*
+ * out[t, n] = base[t, n] + sum_j weights[t, j] * Y[place[t * k + j], n] over the entries j
+ * < k that have a place, added up in fp32 in that order and rounded once.  Y is
+ * [tokens * k, N] as e0m4_matmul_grouped leaves it, base (NULL: zeros) and out [tokens, N], fp16 or bf16; out may be base.
+ */
+int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, const void* plan, int64_t tokens, int k, int64_t groups, const void* base,
+                 void* out, void* stream);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share: for every row m with an adapter a
+ *     out[m] = base[m] + factors[a] * B[a] (A[a] X[m]),
+ * the other rows keep their base.  The layout's entries are the rows, its groups the adapters.  X is [rows, K], base
+ * and out [rows, N], rows x_ld, base_ld and out_ld elements apart; A [adapters, rank, K], B [adapters, N, rank], all
+ * fp16 or bf16; factors fp32 [adapters] (NULL: ones).  base may be NULL (zeros) or out, with the same distance of rows; otherwise
+ * they do not overlap.  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
+ * distances multiples of 8, N <= 2^24, K <= 2^20, X less than 2 GiB.  A X is accumulated in fp32 and multiplied in two 16-bit
+ * parts (22 bits of each row's largest, bf16: 16), the sum with base is rounded once.  Workspace as for e0m4_matmul.
+ */
+size_t e0m4_lora_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K);
+int e0m4_lora(const void* X, int64_t x_ld, int dtype, const void* plan, int64_t rows, int64_t adapters, const void* A, const void* B, int rank,
+              const float* factors, int64_t N, int64_t K, const void* base, int64_t base_ld, void* out, int64_t out_ld, void* workspace,
+              size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostics for tuning sweeps and for tests that force every kernel variant;
  * not needed for normal use.  Sets an integer knob by name (e.g. "gemv_waves");
  * unknown names return E0M4_ERR_SHAPE.  A value of 0 restores the built-in

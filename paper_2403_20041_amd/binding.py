@@ -125,6 +125,21 @@ def lib() -> ctypes.CDLL:
     L.e0m4_kv4_attention.argtypes = [rws, ci, i64, i64, vp, shp, vp, vp, ci, i64, msk, vp, vp, vp, sz, vp]
     L.e0m4_kv4_evict.restype = ci
     L.e0m4_kv4_evict.argtypes = [vp, shp, vp, vp, i64, i64, vp, shp, vp, vp, vp, vp]
+    L.e0m4_groups_bytes.restype = sz
+    L.e0m4_groups_bytes.argtypes = [i64, i64]
+    L.e0m4_groups.restype = ci
+    L.e0m4_groups.argtypes = [vp, i64, i64, vp, vp]
+    L.e0m4_route.restype = ci
+    L.e0m4_route.argtypes = [vp, ci, i64, i64, i64, ci, ci, ci, ctypes.c_float, vp, vp, vp, vp, vp]
+    for name in ("e0m4_matmul_grouped", "e0m8_matmul_grouped", "e0m4_bf16_matmul_grouped"):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [vp, i64, vp, i64, i64, vp, i64, i64, ci, ci, vp, vp]
+    L.e0m4_combine.restype = ci
+    L.e0m4_combine.argtypes = [vp, ci, i64, vp, vp, i64, ci, i64, vp, vp, vp]
+    L.e0m4_lora_workspace_bytes.restype = sz
+    L.e0m4_lora_workspace_bytes.argtypes = [i64, i64, ci, i64, i64]
+    L.e0m4_lora.restype = ci
+    L.e0m4_lora.argtypes = [vp, i64, ci, vp, i64, i64, vp, vp, ci, vp, i64, i64, vp, i64, vp, i64, vp, sz, vp]
     L.e0m4_int4_quantize.restype = ci
     L.e0m4_int4_quantize.argtypes = [vp, i64, i64, ci, vp, vp, vp, vp]
     L.e0m4_int4_dequant.restype = ci
@@ -496,6 +511,184 @@ def e0m4_kv4_evict(cache, shape: E0M4KV4Shape, received, lengths, budget: int, r
     _check(lib().e0m4_kv4_evict(_ptr(cache), s, _ptr(received), _kv4_per_sequence(lengths, shape, "lengths", where), budget, recent,
                                 _ptr(small), o, _ptr(kept), _ptr(lengths_out), _ptr(received_out), _stream(stream)), where)
     return kept, lengths_out, received_out
+
+
+# ---- rows that choose their weights (see include/e0m4.h) ---------------------------------------------
+
+E0M4_ROUTE_SOFTMAX = 0
+E0M4_ROUTE_SIGMOID = 1
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+class E0M4Groups(NamedTuple):
+    """Entries laid out by the weights that they choose: `data` is the library's buffer of int32, the properties are views of it."""
+    data: torch.Tensor
+    rows: int
+    groups: int
+
+    @property
+    def offsets(self) -> torch.Tensor:
+        return self.data[:self.groups + 1]
+
+    @property
+    def order(self) -> torch.Tensor:
+        return self.data[(self.groups + 4) // 4 * 4:][:self.rows]
+
+    @property
+    def place(self) -> torch.Tensor:
+        return self.data[(self.groups + 4) // 4 * 4 + (self.rows + 3) // 4 * 4:][:self.rows]
+
+
+@functools.lru_cache(maxsize=1024)
+def _groups_bytes(rows: int, groups: int) -> int:
+    return lib().e0m4_groups_bytes(rows, groups)
+
+
+def e0m4_groups_bytes(rows: int, groups: int) -> int:
+    return _groups_bytes(rows, groups)
+
+
+def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups:
+    """Memory for the layout of `rows` entries by `groups` weights (uninitialised)."""
+    need = _groups_bytes(rows, groups)
+    if need == 0:
+        raise ValueError("e0m4_groups_alloc: unsupported size: %d rows, %d groups" % (rows, groups))
+    return E0M4Groups(_empty(need // 4, torch.int32, device, stream, "plan"), rows, groups)
+
+
+def _groups_plan(plan, rows, groups, where: str):
+    """The plan's pointer, checked (rows, groups None: any)."""
+    data, r, g = plan
+    need = _groups_bytes(r, g)
+    if need == 0 or data.dtype is not torch.int32 or not data.is_contiguous() or not data.is_cuda or data.numel() * 4 < need or \
+            (rows is not None and r != rows) or (groups is not None and g != groups):
+        raise ValueError("%s: plan must be a layout of %s rows and %s groups on the GPU, got one of %d and %d with %d elements of %s"
+                         % (where, "any" if rows is None else rows, "any" if groups is None else groups, r, g, data.numel(), data.dtype))
+    return data.data_ptr()
+
+
+def e0m4_groups(index: torch.Tensor, groups: int, plan: E0M4Groups = None, stream=None) -> E0M4Groups:
+    """The layout of entries by index (int32, any shape; values outside [0, groups) choose none)."""
+    rows = index.numel()
+    _need(index, torch.int32, index.shape, "index")
+    if plan is None:
+        plan = e0m4_groups_alloc(rows, groups, index.device, stream)
+    _check(lib().e0m4_groups(_ptr(index), rows, groups, _groups_plan(plan, rows, groups, "e0m4_groups"), _stream(stream)), "e0m4_groups")
+    return plan
+
+
+def e0m4_route(logits: torch.Tensor, k: int, scoring: int = E0M4_ROUTE_SOFTMAX, renormalise: bool = True, factor: float = 1.0, count=None,
+               plan: E0M4Groups = None, stream=None):
+    """logits [tokens, experts] (fp16, bf16 or fp32, rows at any distance) -> (chosen int32 [tokens, k], weights fp32 [tokens, k], the
+    entries' layout by expert).  count: int32 [1] on the device, tokens from there on choose none."""
+    tokens, experts = logits.shape
+    if logits.dtype not in _DTYPES:
+        raise TypeError("e0m4_route: logits must be float16, bfloat16 or float32")
+    if not logits.is_cuda or (logits.numel() and experts > 1 and logits.stride(1) != 1):
+        raise ValueError("e0m4_route: logits must be a cuda tensor whose rows are contiguous")
+    if count is not None:
+        _need(count, torch.int32, (1,), "count")
+    device = logits.device
+    if plan is None:
+        plan = e0m4_groups_alloc(tokens * k, experts, device, stream)
+    chosen = _empty((tokens, k), torch.int32, device, stream, "chosen")
+    weights = _empty((tokens, k), torch.float32, device, stream, "weights")
+    _check(lib().e0m4_route(logits.data_ptr(), _DTYPES[logits.dtype], tokens, experts, logits.stride(0), k, scoring, 1 if renormalise else 0, factor,
+                            _ptr(count), chosen.data_ptr(), weights.data_ptr(), _groups_plan(plan, tokens * k, experts, "e0m4_route"),
+                            _stream(stream)), "e0m4_route")
+    return chosen, weights, plan
+
+
+def _matmul_grouped(call: str, codes_bytes, dtype, X, plan, codes, N, K, group, share, epilogue, out, stream):
+    rows, groups = plan.rows, plan.groups
+    pointer = _groups_plan(plan, None, None, call)
+    if share < 0 or (share > 0 and rows % share):
+        raise ValueError("%s: %d entries are not a whole number for each row with share = %d" % (call, rows, share))
+    _need(X, dtype, (rows // share if share else rows, K), "X")
+    need = groups * codes_bytes(N, K, group)
+    if codes.dtype is not torch.uint8 or not codes.is_contiguous() or not codes.is_cuda or codes.numel() < need:
+        raise ValueError("%s: codes must be a contiguous cuda uint8 tensor of at least %d bytes" % (call, need))
+    n_out = N // 2 if epilogue == E0M4_EPILOGUE_SWIGLU else N
+    if out is None:
+        out = _empty((rows, n_out), dtype, X.device, stream, "out")
+    else:
+        _need(out, dtype, (rows, n_out), "out")
+    _check(getattr(lib(), call)(X.data_ptr(), share, pointer, rows, groups, codes.data_ptr(), N, K, group, epilogue, out.data_ptr(), _stream(stream)), call)
+    return out
+
+
+def e0m4_matmul_grouped(X, plan: E0M4Groups, codes, N: int, K: int, group: int, share: int = 0, epilogue: int = E0M4_EPILOGUE_NONE, out=None, stream=None):
+    """Rows of X [rows / share, K] fp16 (share = 0: [rows, K], in the layout's order) times the weights that the layout's entries choose; codes: the packed
+    buffers of all groups one after the other.  Y [rows, N] ([rows, N/2] gated) in the layout's order; see include/e0m4.h."""
+    return _matmul_grouped("e0m4_matmul_grouped", e0m4_codes_bytes, torch.float16, X, plan, codes, N, K, group, share, epilogue, out, stream)
+
+
+def e0m8_matmul_grouped(X, plan: E0M4Groups, codes, N: int, K: int, group: int, share: int = 0, epilogue: int = E0M4_EPILOGUE_NONE, out=None, stream=None):
+    """e0m4_matmul_grouped on 8-bit codes."""
+    return _matmul_grouped("e0m8_matmul_grouped", e0m8_codes_bytes, torch.float16, X, plan, codes, N, K, group, share, epilogue, out, stream)
+
+
+def e0m4_bf16_matmul_grouped(X, plan: E0M4Groups, codes, N: int, K: int, group: int, share: int = 0, epilogue: int = E0M4_EPILOGUE_NONE, out=None,
+                             stream=None):
+    """e0m4_matmul_grouped on bfloat16."""
+    return _matmul_grouped("e0m4_bf16_matmul_grouped", e0m4_codes_bytes, torch.bfloat16, X, plan, codes, N, K, group, share, epilogue, out, stream)
+
+
+def e0m4_combine(Y, weights, plan: E0M4Groups, base=None, out=None, stream=None) -> torch.Tensor:
+    """out [tokens, N] = base + the sum of each token's rows of Y [tokens * k, N] (in the layout's order) times weights fp32 [tokens, k]."""
+    tokens, k = weights.shape
+    N = Y.shape[1]
+    if Y.dtype not in _KV4_DTYPES:
+        raise TypeError("e0m4_combine: Y must be float16 or bfloat16")
+    _need(weights, torch.float32, (tokens, k), "weights")
+    _need(Y, Y.dtype, (tokens * k, N), "Y")
+    if base is not None:
+        _need(base, Y.dtype, (tokens, N), "base")
+    if out is None:
+        out = _empty((tokens, N), Y.dtype, Y.device, stream, "out")
+    else:
+        _need(out, Y.dtype, (tokens, N), "out")
+    _check(lib().e0m4_combine(Y.data_ptr(), _DTYPES[Y.dtype], N, weights.data_ptr(), _groups_plan(plan, tokens * k, None, "e0m4_combine"), tokens, k,
+                              plan.groups, _ptr(base), out.data_ptr(), _stream(stream)), "e0m4_combine")
+    return out
+
+
+def _lora_rows(t, dtype, shape, name: str) -> int:
+    """The distance of the rows of a [rows, columns] tensor whose columns are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.numel() and shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("e0m4_lora: %s must be a cuda %s tensor of shape %s with contiguous rows, got %s %s with strides %s on %s"
+                         % (name, dtype, tuple(shape), t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def e0m4_lora_workspace_bytes(rows: int, adapters: int, rank: int, N: int, K: int) -> int:
+    return lib().e0m4_lora_workspace_bytes(rows, adapters, rank, N, K)
+
+
+def e0m4_lora(X, plan: E0M4Groups, A, B, factors=None, base=None, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """out [rows, N] = base + factors[a] * B[a] (A[a] x) for each row's adapter a, the layout's group of the row; rows of no group keep their base.  X [rows, K],
+    A [adapters, rank, K], B [adapters, N, rank], all fp16 or bf16; X, base and out may be columns of wider matrices; out may be base."""
+    adapters, rank, K = A.shape
+    rows, N, dtype = X.shape[0], B.shape[1], X.dtype
+    if dtype not in _KV4_DTYPES:
+        raise TypeError("e0m4_lora: X must be float16 or bfloat16")
+    x_ld = _lora_rows(X, dtype, (rows, K), "X")
+    _need(A, dtype, (adapters, rank, K), "A")
+    _need(B, dtype, (adapters, N, rank), "B")
+    if factors is not None:
+        _need(factors, torch.float32, (adapters,), "factors")
+    base_ld = _lora_rows(base, dtype, (rows, N), "base") if base is not None else 0
+    if out is None:
+        out = _empty((rows, N), dtype, X.device, stream, "out")
+    out_ld = _lora_rows(out, dtype, (rows, N), "out")
+    if workspace is None:
+        need = e0m4_lora_workspace_bytes(rows, adapters, rank, N, K)
+        if need > 0:
+            workspace = _empty(need, torch.uint8, X.device, stream, "workspace")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().e0m4_lora(X.data_ptr(), x_ld, _DTYPES[dtype], _groups_plan(plan, rows, adapters, "e0m4_lora"), rows, adapters, A.data_ptr(), B.data_ptr(), rank,
+                           _ptr(factors), N, K, _ptr(base), base_ld, out.data_ptr(), out_ld, _ptr(workspace), ws_bytes, _stream(stream)), "e0m4_lora")
+    return out
 
 
 # ---- E0M8, the 8-bit member of the family (see include/e0m4.h) ---------------------------------------

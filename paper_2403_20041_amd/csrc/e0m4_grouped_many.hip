@@ -1,0 +1,416 @@
+// Products of a layout's rows with the quantised weights of their groups, many rows to a group (e0m4_matmul_grouped and its like): tiles of up to
+// 128 rows of one group and 256 weight rows (gated: 128 of the gate and the same of the up projection).
+//     Y[p, n] = sum_k X[row(p), k] * dequant(codes of p's group)[n, k], and with the gated product silu(gate) * up of the two halves of n.
+//
+// Four wavefronts side by side, 64 weight rows each, two workgroups to a compute unit.  Per K slice of 64 (four MFMA sub-steps of 16):
+//   - rows of X come from where the layout's entries say straight to an LDS ring of four stages, two and a half slices ahead, and are read as 16-byte
+//     fragments one sub-step ahead of their use; 128-byte rows whose eight pieces are XOR-swizzled with (row / 2) % 8;
+//   - codes never touch LDS: lane (n = l%32, h = l/32) reads the chunk of row n with k = 32h .. 32h + 31 of the slice ahead of time (8-bit codes: two
+//     chunks), and word s of it is dequantised in registers one sub-step ahead of MFMA s, whose k are {8s..8s+7} and {32+8s..32+8s+7};
+//   - one barrier per slice, after sub-step 1.
+// A tile whose group has fewer rows left is computed in as many 32-row blocks as it has, by a loop of its own: with 128 groups of 256 rows on
+// average a third of the tiles are not whole.
+#include "e0m4_groups.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace e0m4 {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr int BM = 128, BN = 256, BK = 64;
+constexpr int kManyWaves = 4, kManyThreads = kManyWaves * 64;
+constexpr int kRowBytes = BK * 2, kStageBytes = BM * kRowBytes, kStages = 4;
+constexpr int kNumXcd = 8;
+constexpr int TM = BM / 32, TN = 2;
+
+struct ManyArgs {
+    const char* X;
+    const uint4* codes;
+    const GroupTile* tiles;
+    const int* tile_count;
+    const int* order;
+    void* Y;
+    int64_t group_bytes;                        // packed weights of one group
+    uint32_t N, K;
+    uint32_t share, share_reciprocal;           // share 0: rows of X lie in the layout's order
+    uint32_t n_tiles;
+};
+
+template <int FMT, int G, bool GATED>
+__global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs a)
+{
+    constexpr bool E8 = FMT == kGroupedE8, BF = FMT == kGroupedBf16;
+    constexpr int PD = E8 ? 2 : 4, S = kStages, L = S - 1;      // slices of codes in registers, stages of X, how far ahead X is requested
+    constexpr int RP = kManyThreads / 8;                // rows of X per loader pass: one 32-row block
+    constexpr int NCH = E8 ? 2 : 1;
+    static_assert(RP == 32, "a loader pass is a 32-row block");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+
+    // Work items: the tiles of a group, its row tiles first, column after column, so that neighbours share their weights; each XCD takes a
+    // contiguous run of them and shares rows of X and weights in its L2.
+    const uint32_t total = (uint32_t)a.tile_count[0] * a.n_tiles;
+    const uint32_t per_xcd = (total + kNumXcd - 1) / kNumXcd;
+    const uint32_t turn = blockIdx.x / kNumXcd, item = (blockIdx.x % kNumXcd) * per_xcd + turn;
+    if (turn >= per_xcd || item >= total) return;
+    const GroupTile tile = a.tiles[(uint32_t)__builtin_amdgcn_readfirstlane((int)(item / a.n_tiles))];
+    const int group_rows = tile.end - tile.begin;
+    const uint32_t in_group = item - (uint32_t)tile.first_tile * a.n_tiles, m_tiles = (uint32_t)(group_rows + BM - 1) / BM;
+    const uint32_t tile_n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(in_group / m_tiles)), tile_m = in_group - tile_n * m_tiles;
+    const int first = __builtin_amdgcn_readfirstlane(tile.begin + (int)tile_m * BM);
+    const int M = __builtin_amdgcn_readfirstlane(min(BM, tile.end - first));        // rows of this tile
+    const int64_t N = a.N, K = a.K;
+    const int64_t n_out = GATED ? N / 2 : N;
+    const int64_t n0 = (int64_t)tile_n * (GATED ? BN / 2 : BN);
+    const int t = threadIdx.x;
+    const int lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t fmask = frac_mask_vgpr();
+    const PackedLayout<G> lay(E8 ? 2 * K : K);
+    // (4-bit codes fill whole k blocks of two slices; 8-bit codes have a block per slice, and their last pair may lack one)
+    const int slices = E8 ? (int)((K + BK - 1) / BK) : 2 * (int)k_blocks(K);
+    const int kt_end = (slices + 1) & ~1;
+
+    // ---- rows of X: 8 lanes cover one 128-byte row slice; pass p handles row RP * p + t / 8.  Rows that the tile lacks, and k beyond K, are requested
+    // beyond the buffer's end.
+    constexpr uint32_t kNowhere = 0x80000000u;
+    const int a_row = t >> 3, a_piece = (t & 7) ^ ((a_row >> 1) & 7);
+    const char* x_base = a.share ? a.X : a.X + (int64_t)first * K * 2;
+    uint32_t a_off[TM];
+#pragma unroll
+    for (int p = 0; p < TM; ++p) {
+        const int row = a_row + RP * p;
+        uint32_t at = (uint32_t)row;
+        if (a.share && row < M) at = small_quotient((uint32_t)a.order[first + row], a.share_reciprocal);
+        a_off[p] = row < M ? at * (a.K * 2) + (uint32_t)a_piece * 16 : kNowhere;
+    }
+    const uint32_t a_lds_off = (uint32_t)(wave * 8 * kRowBytes);
+
+    // ---- codes: operand block j of this wavefront covers 32 weight rows; gated, block 0 the gate's and block 1 the same of the up projection
+    const int b_h = lane >> 5, b_r = lane & 15;
+    const int64_t nrb = row_blocks(N), rb_tile = n0 / kBlockRows;
+    const uint4* group_codes = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.codes) + (int64_t)tile.group * a.group_bytes);
+    const uint4* b_codes = group_codes + lay.code_index(rb_tile, 0);
+    const uint32_t* b_params = reinterpret_cast<const uint32_t*>(group_codes) + lay.param_index(rb_tile, 0);
+    const uint32_t rb_stride = (uint32_t)lay.nkb * block_bytes(G);
+    uint32_t b_code_off[TN], b_param_off[TN];           // (row blocks beyond the last: that one again, never stored)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        int64_t rb;
+        if (GATED) rb = min(rb_tile + wave * 2 + ((lane >> 4) & 1), nrb / 2 - 1) - rb_tile + j * (nrb / 2);
+        else rb = min(rb_tile + wave * 4 + 2 * j + ((lane >> 4) & 1), nrb - 1) - rb_tile;
+        b_code_off[j] = (uint32_t)rb * rb_stride + (uint32_t)((E8 ? 2 * b_h : b_h) * kBlockRows + b_r) * 16;
+        b_param_off[j] = (uint32_t)rb * rb_stride + (uint32_t)b_r * 4 + (G == 32 ? b_h * 64 : 0);
+    }
+
+    // ---- fragment read position: row 32 i + l%32, piece 4 h + s
+    uint32_t frag_off[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) frag_off[s] = (uint32_t)((lane & 31) * kRowBytes + (((4 * b_h + s) ^ ((lane >> 1) & 7)) << 4));
+
+    u32x4 bset[PD][TN][NCH];
+    uint32_t pwset[PD][TN];
+    half8_t fa[2][TM], fb[2][TN];
+    floatx16 acc[TM][TN];
+
+    // (slices beyond the last are requested through a resource of no bytes: the number of requests stays, memory is not read)
+    auto load_a = [&](auto tm_c, int kt, uint32_t stage_off) {
+        const __amdgpu_buffer_rsrc_t rsrc = rsrc_if(x_base, kt < slices);
+        const uint32_t k0 = (uint32_t)kt * BK;
+        const uint32_t out = (int64_t)k0 + a_piece * 8 >= K ? kNowhere : 0u;
+#pragma unroll
+        for (int p = 0; p < decltype(tm_c)::value; ++p)
+            load_to_lds_b128(rsrc, smem + stage_off + a_lds_off + p * RP * kRowBytes, a_off[p] | out, k0 * 2);
+    };
+    auto load_b = [&](int kt, int set) {
+        const __amdgpu_buffer_rsrc_t code_rsrc = rsrc_if(b_codes, kt < slices), param_rsrc = rsrc_if(b_params, kt < slices);
+        const uint32_t k0 = (uint32_t)kt * BK;
+        const int code_soff = E8 ? (int)((k0 / BK) * kBlockCodeBytes) : (int)((k0 / kCodesPerChunk) * (kBlockRows * 16));
+        const int param_soff = E8 ? (int)((k0 / BK) * (kBlockRows * 4)) : (int)((k0 / G) * (kBlockRows * 4));
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+                bset[set][j][c] = __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, (int)b_code_off[j] + c * kBlockRows * 16, code_soff, 0);
+            pwset[set][j] = __builtin_amdgcn_raw_buffer_load_b32(param_rsrc, (int)b_param_off[j], param_soff, 0);
+        }
+    };
+    auto read_frags = [&](auto tm_c, uint32_t stage_off, int s, half8_t (&dst)[TM]) {
+        const unsigned char* base = smem + stage_off + frag_off[s];
+#pragma unroll
+        for (int i = 0; i < decltype(tm_c)::value; ++i) dst[i] = *reinterpret_cast<const half8_t*>(base + i * 32 * kRowBytes);
+    };
+    auto pair = [](half2_t w1, half2_t bias2, half2_t scale2) -> half2_t { return (w1 - bias2) * scale2; };  // difference exact, product rounded once
+    auto dequant_frags = [&](int set, int s, half8_t (&dst)[TN]) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const half_t sc = param_scale(pwset[set][j]), bi = param_bias(pwset[set][j]);
+            const half2_t s2 = {sc, sc}, b2 = {bi, bi};
+            half2_t o[4];
+            if (E8) {
+                const uint32_t m8 = fmask | (fmask >> 4);       // eight fraction bits of both halves
+#pragma unroll
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    const uint32_t w8 = bset[set][j][(s >> 1) * (NCH - 1)][2 * (s & 1) + h2];
+                    o[2 * h2] = pair(__builtin_bit_cast(half2_t, (w8 & m8) | kExpBits2), b2, s2);
+                    o[2 * h2 + 1] = pair(__builtin_bit_cast(half2_t, (__builtin_amdgcn_alignbit(w8, w8, 8) & m8) | kExpBits2), b2, s2);
+                }
+                dst[j] = *reinterpret_cast<const half8_t*>(o);
+                continue;
+            }
+            const uint32_t word = bset[set][j][0][s];
+            if (BF) {
+                // one fp32 fused multiply-add per weight (products and difference are exact), then one rounding
+                const float sf = __builtin_bit_cast(float, pwset[set][j] << 16);
+                const float nb = -__builtin_bit_cast(float, pwset[set][j] & 0xFFFF0000u) * sf;
+                const half2_t q[4] = {w1_pair<0>(word, fmask), w1_pair<1>(word, fmask), w1_pair<2>(word, fmask), w1_pair<3>(word, fmask)};
+                bf16x2_t ob[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const floatx2 f = {__builtin_fmaf((float)q[p][0], sf, nb), __builtin_fmaf((float)q[p][1], sf, nb)};
+                    ob[p] = __builtin_convertvector(f, bf16x2_t);
+                }
+                dst[j] = *reinterpret_cast<const half8_t*>(ob);
+                continue;
+            }
+            o[0] = pair(w1_pair<0>(word, fmask), b2, s2);
+            o[1] = pair(w1_pair<1>(word, fmask), b2, s2);
+            o[2] = pair(w1_pair<2>(word, fmask), b2, s2);
+            o[3] = pair(w1_pair<3>(word, fmask), b2, s2);
+            dst[j] = *reinterpret_cast<const half8_t*>(o);
+        }
+    };
+    auto mfma_block = [&](auto tm_c, const half8_t (&x)[TM], const half8_t (&w)[TN]) {
+#pragma unroll
+        for (int i = 0; i < decltype(tm_c)::value; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[i][j] = BF ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[i]), __builtin_bit_cast(bf16x8_t, w[j]),
+                                                                         acc[i][j], 0, 0, 0)
+                               : __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i], w[j], acc[i][j], 0, 0, 0);
+    };
+    // After every MFMA some of the instructions that prepare the next sub-step, so that one wavefront keeps the matrix pipe busy.
+    auto interleave = [&](auto tm_c, auto vmem) {
+        constexpr int TMX = decltype(tm_c)::value, kMfma = TMX * TN;
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // one MFMA
+            if (i < TMX) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // one LDS fragment read
+            __builtin_amdgcn_sched_group_barrier(0x002, TMX >= 4 ? 5 : TMX == 3 ? 7 : TMX == 2 ? 9 : 17, 0);      // vector ALU
+            if (i < decltype(vmem)::value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // global load
+        }
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using ILB = std::integral_constant<int, (1 + NCH) * TN>;       // loads of load_b
+
+    auto write_rows = [&](auto tm_c) {
+        using out_t = std::conditional_t<BF, __bf16, half_t>;
+        typedef out_t out8_t __attribute__((ext_vector_type(8)));
+        constexpr int TMX = decltype(tm_c)::value;
+        constexpr int COLS = GATED ? 32 : 64, ROWS = 1024 / COLS, kChunks = TMX * 32 / ROWS;
+        constexpr int PPR = COLS / 8, RPP = 64 / PPR;   // 16-byte pieces per row, rows per pass (two passes per chunk)
+        constexpr int kStride = COLS + 4, NJ = COLS / 32, NR = 16 / NJ;
+        auto value = [&](int i, int r, int j) -> float {
+            if constexpr (GATED) return silu_f32(acc[i][0][r]) * acc[i][1][r];
+            else return acc[i][j][r];
+        };
+        out_t* y = static_cast<out_t*>(a.Y) + (int64_t)first * n_out + n0;
+        const int wcol = wave * COLS, cols = (int)min((int64_t)(GATED ? BN / 2 : BN), n_out - n0);
+        const uint32_t ld = (uint32_t)n_out;
+        if ((n_out & 7) != 0) {                         // rows that are not whole 16-byte pieces: element by element (never gated)
+            const int col0 = wcol + (lane & 31), row0 = 4 * (lane >> 5);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (col0 + 32 * j < cols) {
+#pragma unroll
+                    for (int i = 0; i < TMX; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int row = row0 + 32 * i + 8 * (r >> 2) + (r & 3);
+                            if (row < M) y[(uint32_t)row * ld + (uint32_t)(col0 + 32 * j)] = (out_t)value(i, r, j);
+                        }
+                }
+            }
+            return;
+        }
+        // A wavefront turns 4 KiB of sums at a time around in a piece of LDS of its own (the ring is free by then) and writes whole 16-byte pieces.
+        constexpr uint32_t kTurnBytes = 32 * (32 + 4) * 4;
+        static_assert(kTurnBytes >= 16 * (64 + 4) * 4 && kTurnBytes * kManyWaves <= (uint32_t)kStages * kStageBytes, "fits the stages");
+        float* turn_lds = reinterpret_cast<float*>(smem + wave * kTurnBytes);
+        const int prow = lane / PPR, pcol = (lane % PPR) * 8;
+        const int my_rows = wcol + pcol < cols ? M - prow : 0;
+        const uint32_t o0 = (uint32_t)prow * ld + (uint32_t)(wcol + pcol);
+        __syncthreads();                                // every wavefront has left the K loop's stages
+#pragma unroll
+        for (int ch = 0; ch < kChunks; ++ch) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int rr = 0; rr < NR; ++rr)
+                    turn_lds[(8 * (rr >> 2) + 4 * (lane >> 5) + (rr & 3)) * kStride + 32 * j + (lane & 31)] =
+                        value(ch * ROWS / 32, (ch * ROWS % 32) / 2 + rr, j);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int dr = ch * ROWS + p * RPP;
+                const float* src = turn_lds + (p * RPP + prow) * kStride + pcol;
+                const floatx4 lo = *reinterpret_cast<const floatx4*>(src), hi = *reinterpret_cast<const floatx4*>(src + 4);
+                out8_t o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = (out_t)lo[e];
+                    o[4 + e] = (out_t)hi[e];
+                }
+                if (dr < my_rows) *reinterpret_cast<out8_t*>(y + (o0 + (uint32_t)dr * ld)) = o;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();            // the piece of LDS is read before it is written again
+        }
+    };
+
+    // The tile on TMX 32-row blocks
+    auto run = [&](auto tm_c) {
+        constexpr int TMX = decltype(tm_c)::value, NB = ILB::value;
+#pragma unroll
+        for (int i = 0; i < TMX; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        // One K slice.  On entry: stage `cur` holds slice kt; fa[0], fb[0] hold its sub-step 0 operands; bset[set] holds its codes; the next PD - 1
+        // slices' codes and the next L - 1 slices' rows are in flight.  (REST: one of the last two slices, which request nothing)
+        auto step = [&](auto rest_c, int kt, int set, uint32_t cur, uint32_t nxt, uint32_t last) {
+            constexpr bool REST = decltype(rest_c)::value;
+            read_frags(tm_c, cur, 1, fa[1]);
+            dequant_frags(set, 1, fb[1]);
+            mfma_block(tm_c, fa[0], fb[0]);
+            interleave(tm_c, I0{});
+            __builtin_amdgcn_sched_barrier(0);
+            read_frags(tm_c, cur, 2, fa[0]);
+            dequant_frags(set, 2, fb[0]);
+            mfma_block(tm_c, fa[1], fb[1]);
+            interleave(tm_c, I0{});
+            __builtin_amdgcn_sched_barrier(0);
+            wait_loads<REST ? 0 : (L - 1) * NB + (L - 2) * TMX>();
+            __builtin_amdgcn_s_barrier();   // slice kt+1 is complete in stage `nxt`, and nobody reads slice kt-1 any more
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            read_frags(tm_c, cur, 3, fa[1]);
+            dequant_frags(set, 3, fb[1]);
+            if (!REST) load_a(tm_c, kt + L, last);
+            mfma_block(tm_c, fa[0], fb[0]);
+            interleave(tm_c, I0{});
+            __builtin_amdgcn_sched_barrier(0);
+            if (!REST) load_b(kt + PD, set);
+            read_frags(tm_c, nxt, 0, fa[0]);
+            dequant_frags((set + 1) % PD, 0, fb[0]);
+            mfma_block(tm_c, fa[1], fb[1]);
+            interleave(tm_c, ILB{});
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // (in the order that the loop keeps up: slice kt requests rows L slices on, then codes PD slices on)
+#pragma unroll
+        for (int d = -(PD > L ? PD : L); d < 0; ++d) {
+            if (d + L >= 0) load_a(tm_c, d + L, (uint32_t)(d + L) * kStageBytes);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            if (d + PD >= 0) load_b(d + PD, d + PD);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_loads<(L - 1) * TMX + (PD < L ? PD : L) * NB>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read_frags(tm_c, 0, 0, fa[0]);
+        dequant_frags(0, 0, fb[0]);
+        uint32_t so[S];                                 // stages of slices kt, kt + 1, ..., kt - 1
+#pragma unroll
+        for (int i = 0; i < S; ++i) so[i] = (uint32_t)i * kStageBytes;
+        auto advance_ring = [&]() {                     // by two slices
+            uint32_t tmp[S];
+#pragma unroll
+            for (int i = 0; i < S; ++i) tmp[i] = so[(i + 2) % S];
+#pragma unroll
+            for (int i = 0; i < S; ++i) so[i] = tmp[i];
+        };
+        int kt = 0;
+        for (; kt + PD <= kt_end; kt += PD) {
+#pragma unroll
+            for (int d = 0; d < PD; d += 2) {
+                step(std::false_type{}, kt + d, d, so[0], so[1], so[S - 1]);
+                step(std::false_type{}, kt + d + 1, d + 1, so[1], so[2], so[0]);
+                advance_ring();
+            }
+        }
+        if (PD == 4 && kt < kt_end) {
+            step(std::true_type{}, kt, 0, so[0], so[1], so[S - 1]);
+            step(std::true_type{}, kt + 1, 1, so[1], so[2], so[0]);
+        }
+        wait_loads<0>();                                // (what was requested beyond the range has arrived before the stages are used otherwise)
+        write_rows(tm_c);
+    };
+    if (M > 96) run(std::integral_constant<int, 4>{});
+    else if (M > 64) run(std::integral_constant<int, 3>{});
+    else if (M > 32) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 1>{});
+}
+
+template <int FMT, int G, bool GATED>
+int launch_many(const ManyArgs& a, int64_t tiles, hipStream_t stream)
+{
+    constexpr int lds = kStages * kStageBytes;
+    const int64_t grid = (tiles * a.n_tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
+    if (grid * kManyThreads > 0xffffffffLL) return E0M4_ERR_SHAPE;
+    static std::atomic<uint64_t> lds_allowed{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_many_kernel<FMT, G, GATED>), lds, lds_allowed);
+    if (rc != E0M4_OK) return rc;
+    hipLaunchKernelGGL((grouped_many_kernel<FMT, G, GATED>), dim3((unsigned)grid), dim3(kManyThreads), lds, stream, a);
+    return check_launch();
+}
+
+template <int FMT, int G>
+int launch_many_g(const ManyArgs& a, bool swiglu, int64_t tiles, hipStream_t stream)
+{
+    return swiglu ? launch_many<FMT, G, true>(a, tiles, stream) : launch_many<FMT, G, false>(a, tiles, stream);
+}
+
+}  // namespace
+
+int launch_grouped_many(const GroupedArgs& g, int format, hipStream_t stream)
+{
+    const GroupPlan plan = plan_view(g.plan, g.rows, g.groups);
+    ManyArgs a;
+    a.X = static_cast<const char*>(g.X);
+    a.codes = static_cast<const uint4*>(g.codes);
+    a.tiles = plan.tiles[kTileHeights - 1];
+    a.tile_count = plan.tile_counts + kTileHeights - 1;
+    a.order = plan.order;
+    a.Y = g.Y;
+    a.group_bytes = row_blocks(g.N) * grouped_row_block_bytes(g, format);
+    a.N = (uint32_t)g.N;
+    a.K = (uint32_t)g.K;
+    a.share = (uint32_t)g.share;
+    a.share_reciprocal = small_reciprocal(g.share);
+    const int64_t columns = g.swiglu ? BN / 2 : BN, n_out = g.swiglu ? g.N / 2 : g.N;
+    a.n_tiles = (uint32_t)((n_out + columns - 1) / columns);
+    const int64_t tiles = most_tiles(g.rows, g.groups, BM);
+    if (format == kGroupedE8) return launch_many_g<kGroupedE8, 128>(a, g.swiglu, tiles, stream);
+    auto go = [&](auto fmt_c) -> int {
+        constexpr int FMT = decltype(fmt_c)::value;
+        switch (g.group) {
+            case 32: return launch_many_g<FMT, 32>(a, g.swiglu, tiles, stream);
+            case 64: return launch_many_g<FMT, 64>(a, g.swiglu, tiles, stream);
+            default: return launch_many_g<FMT, 128>(a, g.swiglu, tiles, stream);
+        }
+    };
+    return format == kGroupedBf16 ? go(std::integral_constant<int, kGroupedBf16>{}) : go(std::integral_constant<int, kGroupedFp16>{});
+}
+
+}  // namespace e0m4

@@ -1,0 +1,118 @@
+// Rows laid out by the weights that they choose (e0m4_groups, e0m4_route): the memory of such a layout, and what the kernels that read it need
+// of it.
+#pragma once
+
+#include "e0m4_device.h"
+#include "e0m4_host.h"
+
+namespace e0m4 {
+
+constexpr int64_t kMaxGroupRows = (int64_t)1 << 24;
+constexpr int kMaxGroups = 1023;                // with the group of rows that choose none, one thread of a workgroup each
+constexpr int kMaxChoices = 16;                 // experts of a token
+constexpr int kMaxShare = 255;                  // entries per row of X
+
+// Tiles: rows of one group, so many at most.  A kernel has a workgroup (or several) for every tile of the height that it was built for;
+// how many there are only the device knows, so it is launched for as many as there can be.
+constexpr int kTileHeights = 4;
+constexpr int tile_height(int i) { return 16 << i; }    // 16, 32, 64, 128
+inline int64_t most_tiles(int64_t rows, int64_t groups, int height) { return rows / height + (groups < rows ? groups : rows); }
+
+struct GroupTile {
+    int group;
+    int first_tile;                             // of the group, in this list
+    int begin, end;                             // its rows: positions in the layout
+};
+
+// Layout in memory, in 32-bit words: offsets [groups + 1], order [rows] and place [rows], each padded to a multiple of four words, then
+// the number of tiles of each height, the lists of tiles, and the counts of the first launch's workgroups.
+constexpr int64_t round4(int64_t n) { return (n + 3) & ~(int64_t)3; }
+constexpr int64_t kMaxCountBlocks = 256;
+struct GroupPlan {
+    int* offsets;
+    int* order;
+    int* place;
+    int* tile_counts;
+    GroupTile* tiles[kTileHeights];
+    int* counts;                                // [workgroups][groups + 1]
+};
+inline int64_t plan_words(int64_t rows, int64_t groups)
+{
+    int64_t n = round4(groups + 1) + 2 * round4(rows) + 4;
+    for (int i = 0; i < kTileHeights; ++i) n += 4 * most_tiles(rows, groups, tile_height(i));
+    return n + kMaxCountBlocks * round4(groups + 1);
+}
+inline GroupPlan plan_view(const void* plan, int64_t rows, int64_t groups)
+{
+    int* w = static_cast<int*>(const_cast<void*>(plan));
+    GroupPlan p;
+    p.offsets = w;
+    p.order = p.offsets + round4(groups + 1);
+    p.place = p.order + round4(rows);
+    p.tile_counts = p.place + round4(rows);
+    int* at = p.tile_counts + 4;
+    for (int i = 0; i < kTileHeights; ++i) {
+        p.tiles[i] = reinterpret_cast<GroupTile*>(at);
+        at += 4 * most_tiles(rows, groups, tile_height(i));
+    }
+    p.counts = at;
+    return p;
+}
+
+// x / d for x < 2^24, 1 <= d <= 255: the product with the rounded-up reciprocal is off by less than x / 2^32 < 1 / d.
+inline uint32_t small_reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0; }
+__device__ inline uint32_t small_quotient(uint32_t x, uint32_t reciprocal) { return reciprocal ? __umulhi(x, reciprocal) : x; }
+
+// The expert choice of a router, and the layout (see e0m4.h).  logits null: `experts` is read, one entry per token, and laid out.
+struct RouteArgs {
+    const void* logits;
+    int dtype;
+    int64_t tokens, logits_ld;
+    int groups, k, sigmoid, renormalise;
+    float factor;
+    const int* count;
+    int* experts;
+    float* weights;
+};
+int launch_route(const RouteArgs& a, void* plan, hipStream_t stream);
+int launch_combine(const void* Y, int64_t N, const float* weights, const void* plan, int64_t tokens, int k, int64_t groups, const void* base, void* out,
+                   int dtype, hipStream_t stream);
+
+// Products of the rows of a layout with their groups' weights (see e0m4.h).
+struct GroupedArgs {
+    const void* X;
+    int64_t share;                              // entries per row of X; 0: rows lie in the layout's order
+    const void* plan;
+    int64_t rows, groups;
+    const void* codes;
+    int64_t N, K;
+    int group;
+    bool swiglu;
+    void* Y;
+};
+enum { kGroupedFp16 = 0, kGroupedE8 = 1, kGroupedBf16 = 2 };
+int64_t grouped_row_block_bytes(const GroupedArgs& a, int format);
+int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t stream);      // tiles of 16, 32 or 64 rows
+int launch_grouped_many(const GroupedArgs& a, int format, hipStream_t stream);                 // tiles of 128 rows
+
+// Low-rank adapters of rows (see e0m4.h).
+struct LoraArgs {
+    const void* X;
+    int64_t x_ld;
+    const void* plan;
+    int64_t rows, adapters;
+    const void* A;
+    const void* B;
+    int rank;
+    const float* factors;
+    int64_t N, K;
+    const void* base;
+    int64_t base_ld;
+    void* out;
+    int64_t out_ld;
+    int dtype;
+};
+size_t lora_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K);
+int launch_lora(const LoraArgs& a, void* workspace, hipStream_t stream);
+
+}  // namespace e0m4

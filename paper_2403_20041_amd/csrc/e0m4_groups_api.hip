@@ -1,0 +1,215 @@
+// C entries of the operators of rows that choose their weights: argument checks and the choice of kernels.  Every check happens on the host
+// before anything is enqueued.
+#include "e0m4_groups.h"
+
+namespace e0m4 {
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + b_bytes && q < p + a_bytes;
+}
+
+int check_groups(int64_t rows, int64_t groups)
+{
+    return rows < 0 || rows > kMaxGroupRows || groups < 1 || groups > kMaxGroups ? E0M4_ERR_SHAPE : E0M4_OK;
+}
+
+// Gathered rows of X are reached by 32-bit offsets from its first byte, a gate's up projection from the gate.
+constexpr int64_t kMaxXBytes = 0x7fffffff;
+
+// 8-bit codes: k blocks of 64
+int64_t row_block_bytes(int64_t K, int group, int format)
+{
+    return format == kGroupedE8 ? (K + 63) / 64 * block_bytes(128) : k_blocks(K) * (int64_t)block_bytes(group);
+}
+
+int check_grouped(int64_t rows, int64_t groups, int64_t share, int64_t N, int64_t K, int group, int epilogue, int format)
+{
+    const int rc = check_groups(rows, groups);
+    if (rc != E0M4_OK) return rc;
+    if (format == kGroupedE8 ? group != 64 && group != 128 : group != 32 && group != 64 && group != 128) return E0M4_ERR_GROUP;
+    if (N < 0 || N > (int64_t)1 << 24 || K < 1 || K > (int64_t)1 << (format == kGroupedE8 ? 19 : 20) || K % 32 != 0 || K % group != 0) return E0M4_ERR_SHAPE;
+    if (share < 0 || share > kMaxShare || (share > 0 && rows % share != 0)) return E0M4_ERR_SHAPE;
+    if (epilogue != E0M4_EPILOGUE_NONE && epilogue != E0M4_EPILOGUE_SWIGLU) return E0M4_ERR_SHAPE;
+    if (epilogue == E0M4_EPILOGUE_SWIGLU && (N % 64 != 0 || N / 2 / kBlockRows * row_block_bytes(K, group, format) > kMaxHalfBytes)) return E0M4_ERR_SHAPE;
+    if (share > 0 && rows / share * K * 2 > kMaxXBytes) return E0M4_ERR_SHAPE;
+    return E0M4_OK;
+}
+
+// Tiles of the height nearest to the rows of a group.
+int grouped_height(int64_t rows, int64_t groups)
+{
+    const int64_t each = rows / (groups < rows ? groups : rows);
+    return each <= 12 ? 16 : each <= 24 ? 32 : each <= 48 ? 64 : 128;
+}
+
+int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K, int group,
+                   int epilogue, void* Y, void* stream, int format)
+{
+    const int rc = check_grouped(rows, groups, share, N, K, group, epilogue, format);
+    if (rc != E0M4_OK) return rc;
+    if (rows == 0 || N == 0) return E0M4_OK;
+    if (!X || !plan || !codes || !Y) return E0M4_ERR_NULL;
+    if (!aligned(X, 16) || !aligned(plan, 16) || !aligned(codes, 16) || !aligned(Y, 16)) return E0M4_ERR_ALIGN;
+    GroupedArgs a;
+    a.X = X;
+    a.share = share;
+    a.plan = plan;
+    a.rows = rows;
+    a.groups = groups;
+    a.codes = codes;
+    a.N = N;
+    a.K = K;
+    a.group = group;
+    a.swiglu = epilogue == E0M4_EPILOGUE_SWIGLU;
+    a.Y = Y;
+    const int force = knob(Knob::grouped_tile);
+    const int height = force == 16 || force == 32 || force == 64 || force == 128 ? force : grouped_height(rows, groups);
+    return height == 128 ? launch_grouped_many(a, format, (hipStream_t)stream) : launch_grouped_few(a, format, height, (hipStream_t)stream);
+}
+
+int check_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
+{
+    const int rc = check_groups(rows, adapters);
+    if (rc != E0M4_OK) return rc;
+    if (rank < 8 || rank > 128 || rank % 8 != 0 || N < 0 || N > (int64_t)1 << 24 || N % 8 != 0 || K < 8 || K > (int64_t)1 << 20 || K % 8 != 0) return E0M4_ERR_SHAPE;
+    return E0M4_OK;
+}
+
+}  // namespace
+
+int64_t grouped_row_block_bytes(const GroupedArgs& a, int format) { return row_block_bytes(a.K, a.group, format); }
+
+}  // namespace e0m4
+
+using namespace e0m4;
+
+extern "C" {
+
+size_t e0m4_groups_bytes(int64_t rows, int64_t groups)
+{
+    return check_groups(rows, groups) == E0M4_OK ? (size_t)plan_words(rows, groups) * 4 : 0;
+}
+
+int e0m4_groups(const int32_t* index, int64_t rows, int64_t groups, void* plan, void* stream)
+{
+    const int rc = check_groups(rows, groups);
+    if (rc != E0M4_OK) return rc;
+    if ((!index && rows) || !plan) return E0M4_ERR_NULL;
+    if (!aligned(index, 4) || !aligned(plan, 16)) return E0M4_ERR_ALIGN;
+    RouteArgs a = {};
+    a.tokens = rows;
+    a.groups = (int)groups;
+    a.k = 1;
+    a.experts = const_cast<int32_t*>(index);
+    return launch_route(a, plan, (hipStream_t)stream);
+}
+
+int e0m4_route(const void* logits, int dtype, int64_t tokens, int64_t experts, int64_t logits_ld, int k, int scoring, int renormalise, float factor,
+               const int32_t* count, int32_t* chosen, float* weights, void* plan, void* stream)
+{
+    if (tokens < 0 || experts < 1 || experts > kMaxGroups || k < 1 || k > kMaxChoices || k > experts || tokens > kMaxGroupRows / k) return E0M4_ERR_SHAPE;
+    if (dtype != E0M4_FP16 && dtype != E0M4_BF16 && dtype != E0M4_FP32) return E0M4_ERR_SHAPE;
+    if (scoring != E0M4_ROUTE_SOFTMAX && scoring != E0M4_ROUTE_SIGMOID) return E0M4_ERR_SHAPE;
+    if (logits_ld < 0 || logits_ld > (int64_t)1 << 32) return E0M4_ERR_SHAPE;
+    if (tokens == 0 && !plan) return E0M4_OK;
+    if (tokens && (!logits || !chosen || !weights)) return E0M4_ERR_NULL;
+    if (!aligned(logits, dtype == E0M4_FP32 ? 4 : 2) || !aligned(count, 4) || !aligned(chosen, 4) || !aligned(weights, 4) || !aligned(plan, 16)) return E0M4_ERR_ALIGN;
+    RouteArgs a;
+    a.logits = tokens ? logits : nullptr;
+    a.dtype = dtype;
+    a.tokens = tokens;
+    a.logits_ld = logits_ld;
+    a.groups = (int)experts;
+    a.k = k;
+    a.sigmoid = scoring == E0M4_ROUTE_SIGMOID;
+    a.renormalise = renormalise != 0;
+    a.factor = factor;
+    a.count = count;
+    a.experts = chosen;
+    a.weights = weights;
+    return launch_route(a, plan, (hipStream_t)stream);
+}
+
+int e0m4_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K, int group,
+                        int epilogue, void* Y_f16, void* stream)
+{
+    return matmul_grouped(X_f16, share, plan, rows, groups, codes, N, K, group, epilogue, Y_f16, stream, kGroupedFp16);
+}
+
+int e0m8_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K, int group,
+                        int epilogue, void* Y_f16, void* stream)
+{
+    return matmul_grouped(X_f16, share, plan, rows, groups, codes, N, K, group, epilogue, Y_f16, stream, kGroupedE8);
+}
+
+int e0m4_bf16_matmul_grouped(const void* X_bf16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
+                             int group, int epilogue, void* Y_bf16, void* stream)
+{
+    return matmul_grouped(X_bf16, share, plan, rows, groups, codes, N, K, group, epilogue, Y_bf16, stream, kGroupedBf16);
+}
+
+int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, const void* plan, int64_t tokens, int k, int64_t groups, const void* base,
+                 void* out, void* stream)
+{
+    if (tokens < 0 || k < 1 || k > kMaxShare || tokens > kMaxGroupRows / k || N < 0 || N > (int64_t)1 << 24) return E0M4_ERR_SHAPE;
+    const int rc = check_groups(tokens * k, groups);
+    if (rc != E0M4_OK) return rc;
+    if (dtype != E0M4_FP16 && dtype != E0M4_BF16) return E0M4_ERR_SHAPE;
+    if (tokens == 0 || N == 0) return E0M4_OK;
+    if (!Y || !weights || !plan || !out) return E0M4_ERR_NULL;
+    if (!aligned(Y, 16) || !aligned(weights, 4) || !aligned(plan, 16) || !aligned(base, 16) || !aligned(out, 16)) return E0M4_ERR_ALIGN;
+    const size_t bytes = (size_t)tokens * N * 2;
+    if (overlap(out, bytes, Y, bytes * k) || (base && base != out && overlap(out, bytes, base, bytes))) return E0M4_ERR_SHAPE;
+    return launch_combine(Y, N, weights, plan, tokens, k, groups, base, out, dtype, (hipStream_t)stream);
+}
+
+size_t e0m4_lora_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
+{
+    if (check_lora(rows, adapters, rank, N, K) != E0M4_OK || rows == 0 || N == 0) return 0;
+    return lora_workspace_bytes(rows, adapters, rank, N, K);
+}
+
+int e0m4_lora(const void* X, int64_t x_ld, int dtype, const void* plan, int64_t rows, int64_t adapters, const void* A, const void* B, int rank,
+              const float* factors, int64_t N, int64_t K, const void* base, int64_t base_ld, void* out, int64_t out_ld, void* workspace,
+              size_t workspace_bytes, void* stream)
+{
+    const int rc = check_lora(rows, adapters, rank, N, K);
+    if (rc != E0M4_OK) return rc;
+    if (dtype != E0M4_FP16 && dtype != E0M4_BF16) return E0M4_ERR_SHAPE;
+    if (rows == 0 || N == 0) return E0M4_OK;
+    if (!X || !plan || !A || !B || !out || !workspace) return E0M4_ERR_NULL;
+    if (x_ld < K || out_ld < N || (base && base_ld < N) || x_ld > (int64_t)1 << 24 || out_ld > (int64_t)1 << 32 || base_ld > (int64_t)1 << 32)
+        return E0M4_ERR_SHAPE;
+    if (base == out && base_ld != out_ld) return E0M4_ERR_SHAPE;
+    if (((x_ld | out_ld | (base ? base_ld : 0)) & 7) != 0) return E0M4_ERR_ALIGN;
+    if (!aligned(X, 16) || !aligned(plan, 16) || !aligned(A, 16) || !aligned(B, 16) || !aligned(factors, 4) || !aligned(base, 16) || !aligned(out, 16) ||
+        !aligned(workspace, 16))
+        return E0M4_ERR_ALIGN;
+    if (((rows - 1) * x_ld + K) * 2 > kMaxXBytes) return E0M4_ERR_SHAPE;
+    if (workspace_bytes < lora_workspace_bytes(rows, adapters, rank, N, K)) return E0M4_ERR_WORKSPACE;
+    LoraArgs a;
+    a.X = X;
+    a.x_ld = x_ld;
+    a.plan = plan;
+    a.rows = rows;
+    a.adapters = adapters;
+    a.A = A;
+    a.B = B;
+    a.rank = rank;
+    a.factors = factors;
+    a.N = N;
+    a.K = K;
+    a.base = base;
+    a.base_ld = base ? base_ld : 0;
+    a.out = out;
+    a.out_ld = out_ld;
+    a.dtype = dtype;
+    return launch_lora(a, workspace, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,336 @@
+"""Routing, grouped products, their sum and low-rank adapters against plain forms in 64 bits, at the sizes where they can go wrong."""
+import pytest
+import torch
+
+import groups_plain as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+FORMATS = {"e0m4": torch.float16, "e0m8": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def e0m4():
+    import paper_2403_20041_amd as pkg
+
+    pkg.lib()
+    return pkg
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def check_plan(plan, index, groups):
+    for name, want in zip(("offsets", "order", "place"), plain.layout(index, groups)):
+        assert torch.equal(getattr(plan, name).cpu(), want), name
+
+
+def within(got, want, bound, what=""):
+    err = (got.cpu().double() - want).abs()
+    bad = ~(err <= bound)
+    assert not bad.any(), "%s: %d of %d outside, the worst %g of its bound" % (what, int(bad.sum()), bad.numel(), float((err / bound).max()))
+
+
+# ---- layout and router -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,groups", [(0, 3), (1, 1), (5, 1023), (63, 7), (64, 64), (65, 8), (1024, 128), (1025, 300), (2048, 1), (2049, 60), (5000, 1023),
+                                         (40000, 9)])
+def test_layout(e0m4, rows, groups):
+    g = gen(rows + groups)
+    index = torch.randint(-1, groups + 1, (rows,), generator=g, dtype=torch.int32)
+    if groups > 2:
+        index[index == 1] = 0                          # an empty group, and a fuller one
+    plan = e0m4.e0m4_groups(index.to(DEV), groups)
+    check_plan(plan, index, groups)
+
+
+@pytest.mark.parametrize("value", [0, 2, -1, 5, -2 ** 31, 2 ** 31 - 1])
+def test_layout_of_one_value(e0m4, value):
+    index = torch.full((3000,), value, dtype=torch.int32)
+    check_plan(e0m4.e0m4_groups(index.to(DEV), 5), index, 5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens,experts,k", [(1, 64, 6), (1, 1, 1), (3, 8, 8), (33, 16, 2), (200, 128, 8), (257, 256, 16), (700, 60, 4), (40, 1023, 8)])
+def test_route(e0m4, dtype, tokens, experts, k):
+    g = gen(tokens)
+    wide = (torch.randn((tokens, experts + 5), generator=g) * 2).to(dtype)
+    logits = wide[:, 3:3 + experts]                    # rows at a distance
+    for sigmoid in (False, True):
+        for renormalise in (False, True):
+            count = None if sigmoid else torch.tensor([tokens * 2 // 3], dtype=torch.int32)
+            want, w = plain.route(logits, k, sigmoid, renormalise, 2.5, None if count is None else int(count))
+            chosen, weights, plan = e0m4.e0m4_route(wide.to(DEV)[:, 3:3 + experts], k, scoring=int(sigmoid), renormalise=renormalise, factor=2.5,
+                                                    count=None if count is None else count.to(DEV))
+            assert torch.equal(chosen.cpu(), want)
+            # exponentials good to two steps and to half a step of their argument (below 32), sums over the experts in fp32
+            within(weights, w, w * (experts + 72) * plain.U + 1e-38)
+            check_plan(plan, want, experts)
+
+
+def test_route_of_ties_infinities_and_nan(e0m4):
+    inf, nan = float("inf"), float("nan")
+    logits = torch.zeros((8, 70))
+    logits[1] = torch.arange(70) % 5                   # ties in many lanes
+    logits[2] = -inf
+    logits[3, 40], logits[3, 3] = inf, inf
+    logits[4, 7], logits[4, 8] = nan, 5.0
+    logits[5] = nan
+    logits[6, ::2] = -inf
+    logits[7, 33] = -0.0
+    for sigmoid in (False, True):
+        want, w = plain.route(logits, 4, sigmoid, True)
+        chosen, weights, plan = e0m4.e0m4_route(logits.to(DEV), 4, scoring=int(sigmoid))
+        assert torch.equal(chosen.cpu(), want)
+        within(weights, w, w * 200 * plain.U + 1e-38)
+        check_plan(plan, want, 70)
+
+
+def test_sigmoid_weights_of_unlikely_experts_add_up(e0m4):
+    logits = torch.linspace(-400, -300, 16).repeat(3, 1)
+    want, w = plain.route(logits, 4, True, True)
+    chosen, weights, _ = e0m4.e0m4_route(logits.to(DEV), 4, scoring=e0m4.E0M4_ROUTE_SIGMOID)
+    assert torch.equal(chosen.cpu(), want)
+    within(weights, w, w * 600 * plain.U)              # (arguments of the exponential up to 400 in fp32)
+
+
+# ---- grouped products ------------------------------------------------------------------------------------------------
+
+def make_weights(e0m4, fmt, groups, N, K, group, seed):
+    """codes of all groups, and (values, scales) on the host"""
+    g = gen(seed)
+    quantise, dequant = {"e0m4": (e0m4.e0m4_quantize, lambda c: e0m4.e0m4_dequant(c, None, None, N, K, group)),
+                         "e0m8": (e0m4.e0m8_quantize, lambda c: e0m4.e0m8_dequant(c, N, K, group)),
+                         "bf16": (e0m4.e0m4_bf16_quantize, lambda c: e0m4.e0m4_bf16_dequant(c, N, K, group))}[fmt]
+    codes, values, scales = [], [], []
+    for _ in range(groups):
+        c, s, _ = quantise((torch.randn((N, K), generator=g) * 0.1).to(FORMATS[fmt]).to(DEV), group)
+        codes.append(c)
+        values.append(dequant(c).cpu())
+        scales.append(s.cpu())
+    return torch.stack(codes), torch.stack(values), torch.stack(scales)
+
+
+CASES = [                                              # format, group, N, K, rows of each group, gated
+    ("e0m4", 128, 64, 128, [1], False),
+    ("e0m4", 128, 128, 256, [0, 1, 0, 3], True),
+    ("e0m4", 128, 33, 384, [2, 5, 0], False),           # columns that are no whole blocks, nor 16-byte rows
+    ("e0m4", 64, 80, 448, [16, 17, 1], False),          # K ends inside a k block
+    ("e0m4", 32, 192, 96, [5, 0, 33], True),
+    ("e0m4", 128, 320, 640, [31, 32, 33, 0, 64], True),
+    ("bf16", 128, 72, 512, [7, 70, 1], False),
+    ("bf16", 64, 128, 192, [16, 0, 15], True),
+    ("bf16", 32, 40, 160, [3, 9], False),
+    ("e0m8", 128, 96, 256, [4, 0, 11], False),
+    ("e0m8", 64, 128, 192, [1, 20, 40], True),          # 8-bit codes: an odd number of k blocks
+    ("e0m4", 128, 520, 1024, [100, 129, 0, 1, 97, 65], False),
+    ("e0m4", 128, 576, 256, [128, 256, 30], True),
+    ("bf16", 32, 264, 352, [130, 5], False),
+    ("e0m8", 64, 264, 320, [200, 2], False),
+]
+
+
+@pytest.mark.parametrize("tile", [0, 16, 32, 64, 128])
+@pytest.mark.parametrize("fmt,group,N,K,sizes,gated", CASES)
+def test_products(e0m4, fmt, group, N, K, sizes, gated, tile):
+    g, groups = gen(N + K), len(sizes)
+    codes, values, scales = make_weights(e0m4, fmt, groups, N, K, group, N)
+    index = torch.cat([torch.full((n,), e, dtype=torch.int32) for e, n in enumerate(sizes)] + [torch.full((3,), -1, dtype=torch.int32)])
+    index = index[torch.randperm(len(index), generator=g)]
+    rows, inside = len(index), sum(sizes)
+    plan = e0m4.e0m4_groups(index.to(DEV), groups)
+    _, order, _ = plain.layout(index, groups)
+    groups_of = index[order.long()].tolist()[:inside]
+    X = torch.randn((rows, K), generator=g).to(FORMATS[fmt])
+    call = {"e0m4": e0m4.e0m4_matmul_grouped, "e0m8": e0m4.e0m8_matmul_grouped, "bf16": e0m4.e0m4_bf16_matmul_grouped}[fmt]
+    epilogue = e0m4.E0M4_EPILOGUE_SWIGLU if gated else e0m4.E0M4_EPILOGUE_NONE
+    try:
+        e0m4.e0m4_set_knob("grouped_tile", tile)
+        for share in (0, 1):
+            at = order.long()[:inside] if share else torch.arange(inside)
+            want, bound = plain.products(X, at, groups_of, values, scales, group, gated)
+            poisoned = X.clone()
+            if not share:
+                poisoned[inside:] = float("nan")       # rows of no group are not read into the others
+            out = torch.full((rows, N // 2 if gated else N), 7.0, dtype=FORMATS[fmt], device=DEV)
+            call(poisoned.to(DEV), plan, codes, N, K, group, share=share, epilogue=epilogue, out=out)
+            within(out[:inside], want, bound, "share %d" % share)
+            assert (out[inside:] == 7.0).all()         # rows behind the last are left as they were
+            again = call(poisoned.to(DEV), plan, codes, N, K, group, share=share, epilogue=epilogue)
+            assert torch.equal(again[:inside], out[:inside])
+    finally:
+        e0m4.e0m4_set_knob("grouped_tile", 0)
+
+
+@pytest.mark.parametrize("tile", [16, 128])
+def test_products_of_gathered_rows_that_several_entries_share(e0m4, tile):
+    groups, N, K, tokens, k = 6, 128, 256, 45, 3
+    g = gen(3)
+    codes, values, scales = make_weights(e0m4, "e0m4", groups, N, K, 128, 5)
+    index = torch.stack([torch.randperm(groups, generator=g)[:k] for _ in range(tokens)]).int()
+    plan = e0m4.e0m4_groups(index.to(DEV), groups)
+    _, order, _ = plain.layout(index, groups)
+    X = torch.randn((tokens, K), generator=g).half()
+    want, bound = plain.products(X, order.long() // k, index.flatten()[order.long()].tolist(), values, scales, 128, False)
+    e0m4.e0m4_set_knob("grouped_tile", tile)
+    try:
+        within(e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 128, share=k), want, bound)
+    finally:
+        e0m4.e0m4_set_knob("grouped_tile", 0)
+
+
+@pytest.mark.parametrize("tile", [16, 32, 64, 128])
+def test_nan_and_infinity_stay_in_their_row(e0m4, tile):
+    N, K = 64, 160                                      # (the last k block is not whole: what lies behind a row is the next one's)
+    codes, values, scales = make_weights(e0m4, "e0m4", 2, N, K, 32, 9)
+    index = torch.tensor([0] * 20 + [1] * 13, dtype=torch.int32)
+    plan = e0m4.e0m4_groups(index.to(DEV), 2)
+    X = torch.randn((33, K), generator=gen(2)).half()
+    clean = e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 32, share=1)
+    X[4, 0], X[25, 3], X[32, K - 1] = float("nan"), float("inf"), float("nan")
+    e0m4.e0m4_set_knob("grouped_tile", tile)
+    try:
+        want = e0m4.e0m4_matmul_grouped(torch.where(torch.isfinite(X), X, 0).to(DEV), plan, codes, N, K, 32, share=1)
+        got = e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 32, share=1)
+    finally:
+        e0m4.e0m4_set_knob("grouped_tile", 0)
+    touched = torch.zeros(33, dtype=torch.bool)
+    touched[[4, 25, 32]] = True
+    assert torch.equal(got[~touched.to(DEV)], want[~touched.to(DEV)])
+    assert not torch.isfinite(got[touched.to(DEV)]).all(1).any()
+    assert torch.isfinite(clean).all()
+
+
+# ---- sum of a token's rows -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("tokens,k,N", [(1, 1, 8), (3, 8, 2048), (5, 16, 520), (7, 2, 33), (40, 3, 130), (2, 9, 1)])
+def test_combine(e0m4, dtype, tokens, k, N):
+    g = gen(tokens + N)
+    index = torch.randint(-1, 6, (tokens, k), generator=g, dtype=torch.int32)
+    plan = e0m4.e0m4_groups(index.to(DEV), 5)
+    offsets, _, place = plain.layout(index, 5)
+    Y = torch.randn((tokens * k, N), generator=g).to(dtype)
+    Y[int(offsets[-1]):] = float("nan")                 # rows that no entry has
+    weights = torch.rand((tokens, k), generator=g)
+    base = torch.randn((tokens, N), generator=g).to(dtype)
+    for b in (None, base):
+        want, bound = plain.combine(Y, weights, place, b)
+        out = e0m4.e0m4_combine(Y.to(DEV), weights.to(DEV), plan, base=None if b is None else b.to(DEV))
+        within(out, want, bound)
+    inplace = base.to(DEV)
+    assert e0m4.e0m4_combine(Y.to(DEV), weights.to(DEV), plan, base=inplace, out=inplace) is inplace
+    assert torch.equal(inplace, out)
+
+
+# ---- low-rank adapters -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,adapters,rank,N,K,runs", [(1, 1, 8, 8, 8, False), (1, 3, 16, 264, 1000, False), (20, 7, 24, 72, 136, False), (64, 40, 16, 512, 640, False),
+                                                         (50, 2, 64, 1096, 264, True), (90, 1, 128, 136, 392, True), (200, 3, 32, 320, 128, True),
+                                                         (300, 2, 8, 64, 2056, True), (130, 2, 104, 200, 72, True), (200, 2, 56, 328, 256, True)])
+def test_lora(e0m4, dtype, rows, adapters, rank, N, K, runs):
+    g = gen(rows + rank)
+    index = torch.randint(-1, adapters, (rows,), generator=g, dtype=torch.int32)
+    if runs:
+        index = index.sort().values
+    if rows == 1:
+        index[:] = adapters - 1
+    wide = torch.randn((rows, K + 16), generator=g).to(dtype)
+    A = (torch.randn((adapters, rank, K), generator=g) * K ** -0.5).to(dtype)
+    B = torch.randn((adapters, N, rank), generator=g).to(dtype)
+    factors = torch.rand(adapters, generator=g) + 0.5
+    base = torch.randn((rows, N + 24), generator=g).to(dtype)
+    plan = e0m4.e0m4_groups(index.to(DEV), adapters)
+    X = wide[:, 8:8 + K]
+    Xd, Ad, Bd, Fd = wide.to(DEV)[:, 8:8 + K], A.to(DEV), B.to(DEV), factors.to(DEV)
+    want, bound = plain.lora(X, index, A, B, factors, base[:, 8:8 + N])
+    got = e0m4.e0m4_lora(Xd, plan, Ad, Bd, factors=Fd, base=base.to(DEV)[:, 8:8 + N])
+    within(got, want, bound)
+    none = (index < 0)
+    assert torch.equal(got.cpu()[none], base[:, 8:8 + N][none])
+    # in place, in columns of a wider matrix
+    inplace = base.to(DEV)
+    view = inplace[:, 8:8 + N]
+    e0m4.e0m4_lora(Xd, plan, Ad, Bd, factors=Fd, base=view, out=view)
+    assert torch.equal(view, got)
+    assert torch.equal(inplace.cpu()[:, :8], base[:, :8]) and torch.equal(inplace.cpu()[:, 8 + N:], base[:, 8 + N:])
+    # without base and factors
+    want, bound = plain.lora(X, index, A, B, None, None)
+    got = e0m4.e0m4_lora(Xd, plan, Ad, Bd)
+    within(got, want, bound)
+    assert not got.cpu()[none].any()
+
+
+def test_lora_of_large_small_and_infinite_rows(e0m4):
+    """fp16: A x far outside fp16's range, below it, zero, and rows that hold NaN or an infinity."""
+    K, N, rank = 64, 64, 16
+    g = gen(8)
+    X = torch.randn((6, K), generator=g).half()
+    X[0] *= 20000.0                                     # A x about 1e8
+    X[1] *= 2.0 ** -14
+    X[2] = 0
+    X[4, 5] = float("nan")
+    X[5, 5] = float("inf")
+    A = (torch.randn((1, rank, K), generator=g) * 600).half()
+    B = (torch.randn((1, N, rank), generator=g) * 2.0 ** -10).half()
+    index = torch.zeros(6, dtype=torch.int32)
+    plan = e0m4.e0m4_groups(index.to(DEV), 1)
+    factors = torch.tensor([2.0 ** -6])
+    got = e0m4.e0m4_lora(X.to(DEV), plan, A.to(DEV), B.to(DEV), factors=factors.to(DEV))
+    want, bound = plain.lora(X[:4], index[:4], A, B, factors, None)
+    within(got[:4], want, bound)
+    assert torch.isnan(got[4]).all() and not torch.isfinite(got[5]).any()
+
+
+# ---- as they are used ------------------------------------------------------------------------------------------------
+
+def feed_forward(e0m4, x, logits, k, w1, w2, inner, hidden, out=None):
+    chosen, weights, plan = e0m4.e0m4_route(logits, k)
+    h = e0m4.e0m4_matmul_grouped(x, plan, w1, 2 * inner, hidden, 128, share=k, epilogue=e0m4.E0M4_EPILOGUE_SWIGLU)
+    y = e0m4.e0m4_matmul_grouped(h, plan, w2, hidden, inner, 128)
+    return e0m4.e0m4_combine(y, weights, plan, base=x, out=out)
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 70, 600])
+def test_captured_and_replayed(e0m4, tokens):
+    """The operators together, captured once and replayed on other inputs, with eager calls between the replays."""
+    experts, k, inner, hidden = 8, 2, 128, 256
+    w1, w2 = make_weights(e0m4, "e0m4", experts, 2 * inner, hidden, 128, 1)[0], make_weights(e0m4, "e0m4", experts, hidden, inner, 128, 2)[0]
+    x, logits = torch.zeros((tokens, hidden), dtype=torch.float16, device=DEV), torch.zeros((tokens, experts), device=DEV)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        feed_forward(e0m4, x, logits, k, w1, w2, inner, hidden)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = feed_forward(e0m4, x, logits, k, w1, w2, inner, hidden)
+    for i in range(4):
+        g = gen(i)
+        x.copy_(torch.randn((tokens, hidden), generator=g).half())
+        logits.copy_(torch.randn((tokens, experts), generator=g))
+        want = feed_forward(e0m4, x, logits, k, w1, w2, inner, hidden)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_two_streams_at_once(e0m4):
+    experts, k, inner, hidden, tokens = 8, 2, 128, 256, 300
+    w1, w2 = make_weights(e0m4, "e0m4", experts, 2 * inner, hidden, 128, 1)[0], make_weights(e0m4, "e0m4", experts, hidden, inner, 128, 2)[0]
+    inputs = [(torch.randn((tokens, hidden), generator=gen(i)).half().to(DEV), torch.randn((tokens, experts), generator=gen(9 + i)).to(DEV)) for i in range(2)]
+    want = [feed_forward(e0m4, x, l, k, w1, w2, inner, hidden) for x, l in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(feed_forward(e0m4, *inputs[i], k, w1, w2, inner, hidden))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y in got[i]:
+            assert torch.equal(y, want[i])
