@@ -32,6 +32,7 @@ const char* const kKnobNames[] = {      // in the order of Knob
     "kv4_attention",              // attention over a cache in 4 bits: 1 the kernel for few queries, 2 the one for many, 3 that with 256 rows to a workgroup
     "kv4_chunk",                  // ... tiles of the cache to a workgroup
     "grouped_tile",               // grouped products: rows of a tile (16, 32, 64 or 128)
+    "grouped_exact",
 };
 static_assert(sizeof(kKnobNames) / sizeof(kKnobNames[0]) == (size_t)Knob::count, "a name for each");
 

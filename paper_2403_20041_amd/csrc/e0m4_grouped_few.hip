@@ -24,19 +24,17 @@ constexpr int kFewWaves = 4;
 constexpr int kFewThreads = kFewWaves * 64;
 constexpr int few_weights_ahead(int R) { return R >= 4 ? 2 : R == 2 ? 3 : 4; }      // k blocks of weights that a wavefront has under way
 
+// (as kernel arguments one by one, in registers from the start)
 struct FewArgs {
-    const char* X;
-    const uint4* codes;
-    const GroupTile* tiles;
-    const int* tile_count;
-    const int* order;
+    const void* X;
+    const void* codes;
     void* Y;
-    int64_t group_bytes;                        // packed weights of one group
+    const void* plan;
+    int rows, groups;
     uint32_t N, K;
-    uint32_t share, share_reciprocal;           // share 0: rows of X lie in the layout's order
     uint32_t chunks;                            // workgroups of a tile
-    uint32_t half_blocks;                       // row blocks of the gate (0: no gated product)
-    int group_shift;
+    uint32_t kind;                              // log2 of the codes' group, and 16 times the entries per row of X (0: rows lie in the layout's order)
+    uint32_t share_reciprocal;
 };
 
 template <int N, int I = 0, typename F>
@@ -48,44 +46,52 @@ __device__ inline void for_each_of(F&& f)
     }
 }
 
-// FMT as in GroupedArgs; MT: tiles of 16 rows; EX: groups of 128 in 4 bits, multiplied as the codes' exact values 2 + c/8, with scale and
-// bias applied to the sums of a k block in fp32 (the activations' sum from MFMAs of the same operands with ones): 28 vector instructions
-// per weight operand and 8 per 16 rows where the dequantisation takes 60.
-template <int FMT, int MT, int R, bool EX, bool GATED>
-__global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
+// MT: tiles of 16 rows; R: row blocks.  Every weight is rounded to 16 bits before the product, as the dequant entry points do: a row's result
+// depends on the tile that it falls into only by the order of sums.  (The codes' exact values, with scale and bias applied to a group's sums in
+// fp32, would take 28 instead of 60 vector instructions per weight operand and 4 - 6 % less time, bfloat16 6 - 12 %, and be off by half a step of
+// each weight: 35.0 and 33.1 us for 64 tokens with 8 of 128 experts, gated 1536 x 2048.)
+template <int FMT, int MT, int R, bool GATED>
+__global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(const char* X, const char* codes, void* Y, const void* plan, int rows, int groups, uint32_t N,
+                                                                       uint32_t K, uint32_t chunks, uint32_t kind, uint32_t share_reciprocal)
 {
     constexpr int NP = FMT == kGroupedE8 ? 2 : 4;       // MFMAs per k block
     constexpr int BLK = NP * 32;                        // weights of a row per k block
     constexpr int DW = few_weights_ahead(R);
     constexpr int PPR = NP * 4, RPI = 64 / PPR, RB = PPR * 16, XE = NP;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const uint32_t tile_no = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x / a.chunks)), chunk = blockIdx.x - tile_no * a.chunks;
-    if ((int)tile_no >= a.tile_count[0]) return;
-    const GroupTile tile = a.tiles[tile_no];
+    const GroupPlan lay = plan_view(plan, rows, groups);
+    constexpr int HEIGHT = MT == 1 ? 0 : MT == 2 ? 1 : 2;
+    static_assert(tile_height(HEIGHT) == 16 * MT, "a list of tiles");
+    const uint32_t share = kind >> 4;
+    const int group_shift = (int)(kind & 15);
+    const uint32_t tile_no = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x / chunks)), chunk = blockIdx.x - tile_no * chunks;
+    // (the list has room for a tile that is not there)
+    const GroupTile tile = lay.tiles[HEIGHT][tile_no];
+    if ((int)tile_no >= lay.class_ends[HEIGHT][kTileClasses - 1]) return;
     const int first = tile.begin + ((int)tile_no - tile.first_tile) * (16 * MT);
     const int M = min(16 * MT, tile.end - first);       // rows of this tile
-    const uint32_t K = a.K, N = a.N;
     const int nkb = (int)((K + BLK - 1) / BLK);
-    const int pw = kBlockRows << (7 - a.group_shift);   // parameter words per k block (8-bit codes: 16)
+    const int pw = kBlockRows << (7 - group_shift);   // parameter words per k block (8-bit codes: 16)
     const uint32_t rb_stride = (uint32_t)nkb * (uint32_t)(kBlockCodeBytes + 4 * pw);
 
     const int t = threadIdx.x;
     const int lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n_l = lane & 15, g_l = lane >> 4;
-    const uint32_t fmask = EX && FMT == kGroupedBf16 ? frac_mask_bf16_vgpr() : frac_mask_vgpr();
-    const uint32_t blocks = GATED ? a.half_blocks : (N + kBlockRows - 1) / kBlockRows;      // of a half
+    const uint32_t fmask = frac_mask_vgpr();
+    const uint32_t half_blocks = N / 2 / kBlockRows;
+    const uint32_t blocks = GATED ? half_blocks : (N + kBlockRows - 1) / kBlockRows;      // of a half
     constexpr int RH = GATED ? R / 2 : R;               // row blocks of a half
     const uint32_t rb0 = chunk * RH;
-    const char* wg_base = reinterpret_cast<const char*>(a.codes) + (int64_t)tile.group * a.group_bytes + (uint64_t)rb0 * rb_stride;
+    const char* wg_base = codes + (int64_t)tile.group * ((int64_t)((N + kBlockRows - 1) / kBlockRows) * rb_stride) + (uint64_t)rb0 * rb_stride;
     uint32_t rb_off[R];                                 // (beyond the last: that one again, its sums are not used); gated: gate, up, gate, up
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const uint32_t s = min((uint32_t)(GATED ? r / 2 : r), blocks - 1 - rb0) + (GATED && (r & 1) ? a.half_blocks : 0u);
+        const uint32_t s = min((uint32_t)(GATED ? r / 2 : r), blocks - 1 - rb0) + (GATED && (r & 1) ? half_blocks : 0u);
         rb_off[r] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(s * rb_stride));
     }
     const uint32_t code_voff = lane * 16;
-    const uint32_t param_voff = (uint32_t)nkb * kBlockCodeBytes + 4 * (((g_l * kCodesPerChunk) >> a.group_shift) * kBlockRows + n_l);
+    const uint32_t param_voff = (uint32_t)nkb * kBlockCodeBytes + 4 * (((g_l * kCodesPerChunk) >> group_shift) * kBlockRows + n_l);
     const uint32_t pb = 4 * pw;
     u32x4 c[DW][R];
     uint32_t pwd[DW][R];
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
     // loads: the 16 rows of an operand read fall into 16 different bank groups.
     unsigned char* xl = smem + wave * (MT * 16 * RB);
     auto swizzle = [](int row) -> int { return FMT == kGroupedE8 ? (row >> 1) & 7 : row & 15; };
-    const char* x_base = a.share ? a.X : a.X + (int64_t)first * K * 2;
+    const char* x_base = share ? X : X + (int64_t)first * K * 2;
     constexpr uint32_t kNowhere = 0x80000000u;          // beyond the resource, whatever is added to it
     uint32_t x_voff[MT][XE], x_rd[NP];
     const int last_piece = (int)(K - (uint32_t)(nkb - 1) * BLK) / 8;    // pieces of a row in the last k block
@@ -114,7 +120,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
         for (int i = 0; i < MT; ++i) {
             const int row = 16 * i + e * RPI + lane / PPR;
             uint32_t at = (uint32_t)row;
-            if (a.share && row < M) at = small_quotient((uint32_t)a.order[first + row], a.share_reciprocal);
+            if (share && row < M) at = small_quotient((uint32_t)lay.order[first + row], share_reciprocal);
             x_voff[i][e] = row < M ? at * (K * 2) + (uint32_t)j * 16 : kNowhere;
         }
     }
@@ -175,29 +181,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
         }
         return *reinterpret_cast<const half8_t*>(o);
     };
-    auto exact_codes = [&](const u32x4& cc, int p) -> half8_t {
-        uint32_t o[4];
-        if (FMT == kGroupedBf16) {
-            o[0] = ((cc[p] >> 3) & fmask) | kExpBits2;
-            o[1] = ((cc[p] << 1) & fmask) | kExpBits2;
-            o[2] = ((cc[p] >> 7) & fmask) | kExpBits2;
-            o[3] = (__builtin_amdgcn_alignbit(cc[p], cc[p], 11) & fmask) | kExpBits2;
-        } else {
-            o[0] = w1_pair_bits<0>(cc[p], fmask);
-            o[1] = w1_pair_bits<1>(cc[p], fmask);
-            o[2] = w1_pair_bits<2>(cc[p], fmask);
-            o[3] = w1_pair_bits<3>(cc[p], fmask);
-        }
-        return *reinterpret_cast<const half8_t*>(o);
-    };
     auto mfma = [](const half8_t& x, const half8_t& w, const floatx4& v) -> floatx4 {
         if constexpr (FMT == kGroupedBf16)
             return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, w), v, 0, 0, 0);
         else return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, v, 0, 0, 0);
     };
-    const half_t one = FMT == kGroupedBf16 ? __builtin_bit_cast(half_t, (uint16_t)0x3F80) : (half_t)1.f;
-    const half8_t ones8 = {one, one, one, one, one, one, one, one};
-
     floatx4 acc[R][MT];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -222,32 +210,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
         if (!decltype(rest_c)::value || kb + kFewWaves < nkb) load_x(kb + kFewWaves);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (EX) {
-            floatx4 sx[MT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) sx[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) sx[i] = mfma(xa[p][i], ones8, sx[i]);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                floatx4 s[MT];
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const half8_t w = exact_codes(c[u % DW][r], p);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) s[i] = mfma(xa[p][i], w, p == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[i]);
-                }
-                const uint32_t pw1 = pwd[u % DW][r];
-                const float sc = FMT == kGroupedBf16 ? __builtin_bit_cast(float, pw1 << 16) : (float)param_scale(pw1);
-                const float bi = FMT == kGroupedBf16 ? __builtin_bit_cast(float, pw1 & 0xFFFF0000u) : (float)param_bias(pw1);
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[r][i][e] += sc * (s[i][e] - bi * sx[i][e]);
-            }
-        } else {
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
 #pragma unroll
@@ -257,7 +219,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
                     for (int i = 0; i < MT; ++i) acc[r][i] = mfma(xa[p][i], w, acc[r][i]);
                 }
             }
-        }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         load_w(kb + DW * kFewWaves, u % DW);
@@ -304,76 +265,62 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(FewArgs a)
             const int m = 16 * i + 4 * (l >> 4) + e;
             if (m >= M) continue;
             const int64_t at = (int64_t)(first + m) * n_out + col;
-            if (FMT == kGroupedBf16) static_cast<__bf16*>(a.Y)[at] = (__bf16)v[e];
-            else static_cast<half_t*>(a.Y)[at] = (half_t)v[e];
+            if (FMT == kGroupedBf16) static_cast<__bf16*>(Y)[at] = (__bf16)v[e];
+            else static_cast<half_t*>(Y)[at] = (half_t)v[e];
         }
     }
 }
 
-template <int FMT, int MT, int R, bool EX, bool GATED>
+template <int FMT, int MT, int R, bool GATED>
 int launch_few(const FewArgs& f, int64_t tiles, hipStream_t stream)
 {
     constexpr int lds = std::max(kFewWaves * R * MT * 64 * 16, kFewWaves * MT * 16 * (FMT == kGroupedE8 ? 128 : 256));
     FewArgs a = f;
-    const uint32_t blocks = GATED ? a.half_blocks : (uint32_t)row_blocks(a.N);
+    const uint32_t blocks = GATED ? a.N / 2 / kBlockRows : (uint32_t)row_blocks(a.N);
     constexpr uint32_t RH = GATED ? R / 2 : R;
     a.chunks = (blocks + RH - 1) / RH;
     const int64_t grid = tiles * a.chunks;
     if (grid * kFewThreads > 0xffffffffLL) return E0M4_ERR_SHAPE;
     static std::atomic<uint64_t> lds_allowed{0};
-    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_few_kernel<FMT, MT, R, EX, GATED>), lds, lds_allowed);
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_few_kernel<FMT, MT, R, GATED>), lds, lds_allowed);
     if (rc != E0M4_OK) return rc;
-    hipLaunchKernelGGL((grouped_few_kernel<FMT, MT, R, EX, GATED>), dim3((unsigned)grid), dim3(kFewThreads), lds, stream, a);
+    hipLaunchKernelGGL((grouped_few_kernel<FMT, MT, R, GATED>), dim3((unsigned)grid), dim3(kFewThreads), lds, stream, static_cast<const char*>(a.X),
+                       static_cast<const char*>(a.codes), a.Y, a.plan, a.rows, a.groups, a.N, a.K, a.chunks, a.kind, a.share_reciprocal);
     return check_launch();
 }
 
-template <int FMT, bool EX, bool GATED>
+template <int FMT, bool GATED>
 int launch_few_as(const FewArgs& f, int64_t tiles, int height, hipStream_t stream)
 {
+    const int r = knob(Knob::grouped_exact);
     switch (height) {
-        case 16: return launch_few<FMT, 1, 4, EX, GATED>(f, tiles, stream);
-        case 32: return launch_few<FMT, 2, 4, EX, GATED>(f, tiles, stream);
-        case 64: return launch_few<FMT, 4, 2, EX, GATED>(f, tiles, stream);
+        case 16: return r == 1 ? launch_few<FMT, 1, 2, GATED>(f, tiles, stream) : launch_few<FMT, 1, 4, GATED>(f, tiles, stream);
+        case 32: return r == 1 ? launch_few<FMT, 2, 2, GATED>(f, tiles, stream) : launch_few<FMT, 2, 4, GATED>(f, tiles, stream);
+        case 64: return r == 1 ? launch_few<FMT, 4, 4, GATED>(f, tiles, stream) : launch_few<FMT, 4, 2, GATED>(f, tiles, stream);
         default: return E0M4_ERR_SHAPE;
     }
-}
-
-template <int FMT, bool GATED>
-int launch_few_ex(const FewArgs& f, int64_t tiles, int height, bool exact, hipStream_t stream)
-{
-    if constexpr (FMT != kGroupedE8) {
-        if (exact) return launch_few_as<FMT, true, GATED>(f, tiles, height, stream);
-    }
-    return launch_few_as<FMT, false, GATED>(f, tiles, height, stream);
 }
 
 }  // namespace
 
 int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t stream)
 {
-    const GroupPlan plan = plan_view(a.plan, a.rows, a.groups);
-    int i = 0;
-    while (tile_height(i) != height) ++i;
     FewArgs f;
-    f.X = static_cast<const char*>(a.X);
-    f.codes = static_cast<const uint4*>(a.codes);
-    f.tiles = plan.tiles[i];
-    f.tile_count = plan.tile_counts + i;
-    f.order = plan.order;
+    f.X = a.X;
+    f.codes = a.codes;
     f.Y = a.Y;
-    f.group_bytes = row_blocks(a.N) * grouped_row_block_bytes(a, format);
+    f.plan = a.plan;
+    f.rows = (int)a.rows;
+    f.groups = (int)a.groups;
     f.N = (uint32_t)a.N;
     f.K = (uint32_t)a.K;
-    f.share = (uint32_t)a.share;
-    f.share_reciprocal = small_reciprocal(a.share);
     f.chunks = 0;
-    f.half_blocks = a.swiglu ? (uint32_t)(a.N / 2 / kBlockRows) : 0;
-    f.group_shift = format == kGroupedE8 || a.group == 128 ? 7 : a.group == 64 ? 6 : 5;
+    f.kind = (uint32_t)a.share << 4 | (format == kGroupedE8 || a.group == 128 ? 7 : a.group == 64 ? 6 : 5);
+    f.share_reciprocal = small_reciprocal(a.share);
     const int64_t tiles = most_tiles(a.rows, a.groups, height);
-    const bool exact = a.group == 128;
     auto go = [&](auto fmt_c) -> int {
         constexpr int FMT = decltype(fmt_c)::value;
-        return a.swiglu ? launch_few_ex<FMT, true>(f, tiles, height, exact, stream) : launch_few_ex<FMT, false>(f, tiles, height, exact, stream);
+        return a.swiglu ? launch_few_as<FMT, true>(f, tiles, height, stream) : launch_few_as<FMT, false>(f, tiles, height, stream);
     };
     switch (format) {
         case kGroupedFp16: return go(std::integral_constant<int, kGroupedFp16>{});

@@ -24,78 +24,101 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
-constexpr int BM = 128, BN = 256, BK = 64;
-constexpr int kManyWaves = 4, kManyThreads = kManyWaves * 64;
-constexpr int kRowBytes = BK * 2, kStageBytes = BM * kRowBytes, kStages = 4;
+constexpr int BK = 64;
+constexpr int kRowBytes = BK * 2, kStages = 4;
 constexpr int kNumXcd = 8;
-constexpr int TM = BM / 32, TN = 2;
+constexpr int TN = 2;                           // operand blocks of 32 weight rows per wavefront
 
+// (as kernel arguments one by one, in registers from the start)
 struct ManyArgs {
-    const char* X;
-    const uint4* codes;
-    const GroupTile* tiles;
-    const int* tile_count;
-    const int* order;
+    const void* X;
+    const void* codes;
     void* Y;
-    int64_t group_bytes;                        // packed weights of one group
+    const void* plan;
+    int rows, groups;
     uint32_t N, K;
-    uint32_t share, share_reciprocal;           // share 0: rows of X lie in the layout's order
     uint32_t n_tiles;
+    uint32_t share, share_reciprocal;           // share 0: rows of X lie in the layout's order
 };
 
-template <int FMT, int G, bool GATED>
-__global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs a)
+// A tile is 32 TM rows and 64 WN columns; KS groups of WN wavefronts take a part of K each, and their sums are added in LDS.
+template <int FMT, int G, bool GATED, int TM, int WN, int KS>
+__global__ __launch_bounds__(64 * WN * KS, 2) void grouped_many_kernel(const char* X, const char* codes, void* Y, const void* plan, int rows, int groups,
+                                                                               uint32_t N32, uint32_t K32, uint32_t n_tiles, uint32_t share,
+                                                                               uint32_t share_reciprocal)
 {
+    const GroupPlan lists = plan_view(plan, rows, groups);
+    constexpr int HEIGHT = TM == 4 ? 3 : 2;
+    static_assert(tile_height(HEIGHT) == 32 * TM, "a list of tiles");
+    constexpr int BM = 32 * TM, BN = 64 * WN;
+    constexpr int kThreads = 64 * WN;                   // of a part of K
+    constexpr int kStageBytes = BM * kRowBytes;
     constexpr bool E8 = FMT == kGroupedE8, BF = FMT == kGroupedBf16;
     constexpr int PD = E8 ? 2 : 4, S = kStages, L = S - 1;      // slices of codes in registers, stages of X, how far ahead X is requested
-    constexpr int RP = kManyThreads / 8;                // rows of X per loader pass: one 32-row block
+    constexpr int RP = kThreads / 8;                    // rows of X per loader pass
+    constexpr int PA = BM / RP;                         // passes
     constexpr int NCH = E8 ? 2 : 1;
-    static_assert(RP == 32, "a loader pass is a 32-row block");
+    static_assert(32 % RP == 0, "a 32-row block is whole loader passes");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
-    // Work items: the tiles of a group, its row tiles first, column after column, so that neighbours share their weights; each XCD takes a
-    // contiguous run of them and shares rows of X and weights in its L2.
-    const uint32_t total = (uint32_t)a.tile_count[0] * a.n_tiles;
-    const uint32_t per_xcd = (total + kNumXcd - 1) / kNumXcd;
-    const uint32_t turn = blockIdx.x / kNumXcd, item = (blockIdx.x % kNumXcd) * per_xcd + turn;
-    if (turn >= per_xcd || item >= total) return;
-    const GroupTile tile = a.tiles[(uint32_t)__builtin_amdgcn_readfirstlane((int)(item / a.n_tiles))];
-    const int group_rows = tile.end - tile.begin;
-    const uint32_t in_group = item - (uint32_t)tile.first_tile * a.n_tiles, m_tiles = (uint32_t)(group_rows + BM - 1) / BM;
+    // Work items: class after class, in each the tiles of a group, its row tiles first, column after column, so that neighbours share their weights.
+    // Each XCD takes a contiguous run of every class and shares rows of X and weights in its L2.
+    const uint32_t xcd = blockIdx.x % kNumXcd;
+    uint32_t turn = blockIdx.x / kNumXcd, from = 0, item = 0;
+    bool found = false;
+#pragma unroll
+    for (int c = 0; c < kTileClasses; ++c) {
+        const uint32_t to = (uint32_t)lists.class_ends[HEIGHT][c] * n_tiles, each = (to - from + kNumXcd - 1) / kNumXcd;
+        if (!found && turn < each) {
+            item = from + xcd * each + turn;
+            found = true;
+            if (item >= to) return;
+        }
+        turn -= found ? 0 : each;
+        from = to;
+    }
+    if (!found) return;
+    const GroupTile tile = lists.tiles[HEIGHT][(uint32_t)__builtin_amdgcn_readfirstlane((int)(item / n_tiles))];
+    const int group_rows = tile.end - tile.begin;       // (those of its tiles of this class)
+    const uint32_t in_group = item - (uint32_t)tile.first_tile * n_tiles, m_tiles = (uint32_t)(group_rows + BM - 1) / BM;
     const uint32_t tile_n = (uint32_t)__builtin_amdgcn_readfirstlane((int)(in_group / m_tiles)), tile_m = in_group - tile_n * m_tiles;
     const int first = __builtin_amdgcn_readfirstlane(tile.begin + (int)tile_m * BM);
     const int M = __builtin_amdgcn_readfirstlane(min(BM, tile.end - first));        // rows of this tile
-    const int64_t N = a.N, K = a.K;
+    const int64_t N = N32, K = K32;
     const int64_t n_out = GATED ? N / 2 : N;
     const int64_t n0 = (int64_t)tile_n * (GATED ? BN / 2 : BN);
-    const int t = threadIdx.x;
+    const int part = KS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads) : 0;
+    const int t = KS > 1 ? (int)threadIdx.x % kThreads : (int)threadIdx.x;
     const int lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const uint32_t fmask = frac_mask_vgpr();
     const PackedLayout<G> lay(E8 ? 2 * K : K);
     // (4-bit codes fill whole k blocks of two slices; 8-bit codes have a block per slice, and their last pair may lack one)
     const int slices = E8 ? (int)((K + BK - 1) / BK) : 2 * (int)k_blocks(K);
-    const int kt_end = (slices + 1) & ~1;
+    const int pairs = (slices + 1) / 2;
+    const int kt_begin = KS > 1 ? __builtin_amdgcn_readfirstlane(2 * (pairs * part / KS)) : 0;
+    const int kt_end = KS > 1 ? __builtin_amdgcn_readfirstlane(2 * (pairs * (part + 1) / KS)) : 2 * pairs;
+    const int kt_last = KS > 1 ? min(kt_end, slices) : slices;
 
     // ---- rows of X: 8 lanes cover one 128-byte row slice; pass p handles row RP * p + t / 8.  Rows that the tile lacks, and k beyond K, are requested
     // beyond the buffer's end.
     constexpr uint32_t kNowhere = 0x80000000u;
     const int a_row = t >> 3, a_piece = (t & 7) ^ ((a_row >> 1) & 7);
-    const char* x_base = a.share ? a.X : a.X + (int64_t)first * K * 2;
-    uint32_t a_off[TM];
+    const char* x_base = share ? X : X + (int64_t)first * K * 2;
+    uint32_t a_off[PA];
 #pragma unroll
-    for (int p = 0; p < TM; ++p) {
+    for (int p = 0; p < PA; ++p) {
         const int row = a_row + RP * p;
         uint32_t at = (uint32_t)row;
-        if (a.share && row < M) at = small_quotient((uint32_t)a.order[first + row], a.share_reciprocal);
-        a_off[p] = row < M ? at * (a.K * 2) + (uint32_t)a_piece * 16 : kNowhere;
+        if (share && row < M) at = small_quotient((uint32_t)lists.order[first + row], share_reciprocal);
+        a_off[p] = row < M ? at * (K32 * 2) + (uint32_t)a_piece * 16 : kNowhere;
     }
     const uint32_t a_lds_off = (uint32_t)(wave * 8 * kRowBytes);
 
     // ---- codes: operand block j of this wavefront covers 32 weight rows; gated, block 0 the gate's and block 1 the same of the up projection
     const int b_h = lane >> 5, b_r = lane & 15;
     const int64_t nrb = row_blocks(N), rb_tile = n0 / kBlockRows;
-    const uint4* group_codes = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.codes) + (int64_t)tile.group * a.group_bytes);
+    const uint4* group_codes = reinterpret_cast<const uint4*>(codes + (int64_t)tile.group * (nrb * lay.nkb * block_bytes(G)));
     const uint4* b_codes = group_codes + lay.code_index(rb_tile, 0);
     const uint32_t* b_params = reinterpret_cast<const uint32_t*>(group_codes) + lay.param_index(rb_tile, 0);
     const uint32_t rb_stride = (uint32_t)lay.nkb * block_bytes(G);
@@ -121,15 +144,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
 
     // (slices beyond the last are requested through a resource of no bytes: the number of requests stays, memory is not read)
     auto load_a = [&](auto tm_c, int kt, uint32_t stage_off) {
-        const __amdgpu_buffer_rsrc_t rsrc = rsrc_if(x_base, kt < slices);
+        const __amdgpu_buffer_rsrc_t rsrc = rsrc_if(x_base, kt < kt_last);
         const uint32_t k0 = (uint32_t)kt * BK;
         const uint32_t out = (int64_t)k0 + a_piece * 8 >= K ? kNowhere : 0u;
 #pragma unroll
-        for (int p = 0; p < decltype(tm_c)::value; ++p)
+        for (int p = 0; p < decltype(tm_c)::value * 32 / RP; ++p)
             load_to_lds_b128(rsrc, smem + stage_off + a_lds_off + p * RP * kRowBytes, a_off[p] | out, k0 * 2);
     };
     auto load_b = [&](int kt, int set) {
-        const __amdgpu_buffer_rsrc_t code_rsrc = rsrc_if(b_codes, kt < slices), param_rsrc = rsrc_if(b_params, kt < slices);
+        const __amdgpu_buffer_rsrc_t code_rsrc = rsrc_if(b_codes, kt < kt_last), param_rsrc = rsrc_if(b_params, kt < kt_last);
         const uint32_t k0 = (uint32_t)kt * BK;
         const int code_soff = E8 ? (int)((k0 / BK) * kBlockCodeBytes) : (int)((k0 / kCodesPerChunk) * (kBlockRows * 16));
         const int param_soff = E8 ? (int)((k0 / BK) * (kBlockRows * 4)) : (int)((k0 / G) * (kBlockRows * 4));
@@ -220,7 +243,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
             if constexpr (GATED) return silu_f32(acc[i][0][r]) * acc[i][1][r];
             else return acc[i][j][r];
         };
-        out_t* y = static_cast<out_t*>(a.Y) + (int64_t)first * n_out + n0;
+        out_t* y = static_cast<out_t*>(Y) + (int64_t)first * n_out + n0;
         const int wcol = wave * COLS, cols = (int)min((int64_t)(GATED ? BN / 2 : BN), n_out - n0);
         const uint32_t ld = (uint32_t)n_out;
         if ((n_out & 7) != 0) {                         // rows that are not whole 16-byte pieces: element by element (never gated)
@@ -241,12 +264,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
         }
         // A wavefront turns 4 KiB of sums at a time around in a piece of LDS of its own (the ring is free by then) and writes whole 16-byte pieces.
         constexpr uint32_t kTurnBytes = 32 * (32 + 4) * 4;
-        static_assert(kTurnBytes >= 16 * (64 + 4) * 4 && kTurnBytes * kManyWaves <= (uint32_t)kStages * kStageBytes, "fits the stages");
+        static_assert(kTurnBytes >= 16 * (64 + 4) * 4 && kTurnBytes * WN <= (uint32_t)KS * kStages * kStageBytes, "fits the stages");
         float* turn_lds = reinterpret_cast<float*>(smem + wave * kTurnBytes);
         const int prow = lane / PPR, pcol = (lane % PPR) * 8;
         const int my_rows = wcol + pcol < cols ? M - prow : 0;
         const uint32_t o0 = (uint32_t)prow * ld + (uint32_t)(wcol + pcol);
-        __syncthreads();                                // every wavefront has left the K loop's stages
+        __syncthreads();                                // every wavefront has left the K loop's stages (or the other parts' sums)
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
 #pragma unroll
@@ -277,7 +300,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
 
     // The tile on TMX 32-row blocks
     auto run = [&](auto tm_c) {
-        constexpr int TMX = decltype(tm_c)::value, NB = ILB::value;
+        constexpr int TMX = decltype(tm_c)::value, PAX = TMX * 32 / RP, NB = ILB::value;
+        const uint32_t ring = (uint32_t)part * S * kStageBytes;
 #pragma unroll
         for (int i = 0; i < TMX; ++i)
 #pragma unroll
@@ -298,7 +322,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
             mfma_block(tm_c, fa[1], fb[1]);
             interleave(tm_c, I0{});
             __builtin_amdgcn_sched_barrier(0);
-            wait_loads<REST ? 0 : (L - 1) * NB + (L - 2) * TMX>();
+            wait_loads<REST ? 0 : (L - 1) * NB + (L - 2) * PAX>();
             __builtin_amdgcn_s_barrier();   // slice kt+1 is complete in stage `nxt`, and nobody reads slice kt-1 any more
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
@@ -318,21 +342,21 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
         // (in the order that the loop keeps up: slice kt requests rows L slices on, then codes PD slices on)
 #pragma unroll
         for (int d = -(PD > L ? PD : L); d < 0; ++d) {
-            if (d + L >= 0) load_a(tm_c, d + L, (uint32_t)(d + L) * kStageBytes);
+            if (d + L >= 0) load_a(tm_c, kt_begin + d + L, ring + (uint32_t)(d + L) * kStageBytes);
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            if (d + PD >= 0) load_b(d + PD, d + PD);
+            if (d + PD >= 0) load_b(kt_begin + d + PD, d + PD);
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
         }
-        wait_loads<(L - 1) * TMX + (PD < L ? PD : L) * NB>();
+        wait_loads<(L - 1) * PAX + (PD < L ? PD : L) * NB>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read_frags(tm_c, 0, 0, fa[0]);
+        read_frags(tm_c, ring, 0, fa[0]);
         dequant_frags(0, 0, fb[0]);
         uint32_t so[S];                                 // stages of slices kt, kt + 1, ..., kt - 1
 #pragma unroll
-        for (int i = 0; i < S; ++i) so[i] = (uint32_t)i * kStageBytes;
+        for (int i = 0; i < S; ++i) so[i] = ring + (uint32_t)i * kStageBytes;
         auto advance_ring = [&]() {                     // by two slices
             uint32_t tmp[S];
 #pragma unroll
@@ -340,7 +364,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
 #pragma unroll
             for (int i = 0; i < S; ++i) so[i] = tmp[i];
         };
-        int kt = 0;
+        int kt = kt_begin;
         for (; kt + PD <= kt_end; kt += PD) {
 #pragma unroll
             for (int d = 0; d < PD; d += 2) {
@@ -354,63 +378,103 @@ __global__ __launch_bounds__(kManyThreads, 2) void grouped_many_kernel(ManyArgs 
             step(std::true_type{}, kt + 1, 1, so[1], so[2], so[0]);
         }
         wait_loads<0>();                                // (what was requested beyond the range has arrived before the stages are used otherwise)
+        if constexpr (KS > 1) {
+            // The parts' sums are added to the first's, in the order of K, through LDS.  Parts of one pair of slices fewer wait at the barriers of
+            // two steps more.
+            if (kt_end - kt_begin < 2 * ((pairs + KS - 1) / KS)) {
+                __syncthreads();
+                __syncthreads();
+            }
+            __syncthreads();                            // every wavefront has left the K loop's stages
+            floatx4* sums = reinterpret_cast<floatx4*>(smem);
+            constexpr int kPart = TMX * TN * 4 * kThreads;
+            static_assert((KS - 1) * TM * TN * 4 * kThreads * 16 <= KS * kStages * kStageBytes, "fits the stages");
+            if (part > 0) {
+#pragma unroll
+                for (int i = 0; i < TMX; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            sums[(part - 1) * kPart + ((i * TN + j) * 4 + q) * kThreads + t] =
+                                floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            }
+            __syncthreads();
+            if (part > 0) return;
+#pragma unroll
+            for (int s = 0; s < KS - 1; ++s)
+#pragma unroll
+                for (int i = 0; i < TMX; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const floatx4 v = sums[s * kPart + ((i * TN + j) * 4 + q) * kThreads + t];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[e];
+                        }
+        }
         write_rows(tm_c);
     };
-    if (M > 96) run(std::integral_constant<int, 4>{});
-    else if (M > 64) run(std::integral_constant<int, 3>{});
-    else if (M > 32) run(std::integral_constant<int, 2>{});
+    if constexpr (TM >= 4) {
+        if (M > 96) return run(std::integral_constant<int, 4>{});
+        if (M > 64) return run(std::integral_constant<int, 3>{});
+    }
+    if (M > 32) run(std::integral_constant<int, 2>{});
     else run(std::integral_constant<int, 1>{});
 }
 
-template <int FMT, int G, bool GATED>
-int launch_many(const ManyArgs& a, int64_t tiles, hipStream_t stream)
+template <int FMT, int G, bool GATED, int TM, int WN, int KS>
+int launch_many(const ManyArgs& f, int64_t rows, int64_t groups, hipStream_t stream)
 {
-    constexpr int lds = kStages * kStageBytes;
-    const int64_t grid = (tiles * a.n_tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
-    if (grid * kManyThreads > 0xffffffffLL) return E0M4_ERR_SHAPE;
+    constexpr int lds = KS * kStages * 32 * TM * kRowBytes, threads = 64 * WN * KS;
+    ManyArgs a = f;
+    const int64_t columns = GATED ? 32 * WN : 64 * WN, n_out = GATED ? a.N / 2 : a.N;
+    a.n_tiles = (uint32_t)((n_out + columns - 1) / columns);
+    const int64_t grid = (most_tiles(rows, groups, 32 * TM) * a.n_tiles / kNumXcd + kTileClasses) * kNumXcd;
+    if (grid * threads > 0xffffffffLL) return E0M4_ERR_SHAPE;
     static std::atomic<uint64_t> lds_allowed{0};
-    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_many_kernel<FMT, G, GATED>), lds, lds_allowed);
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_many_kernel<FMT, G, GATED, TM, WN, KS>), lds, lds_allowed);
     if (rc != E0M4_OK) return rc;
-    hipLaunchKernelGGL((grouped_many_kernel<FMT, G, GATED>), dim3((unsigned)grid), dim3(kManyThreads), lds, stream, a);
+    hipLaunchKernelGGL((grouped_many_kernel<FMT, G, GATED, TM, WN, KS>), dim3((unsigned)grid), dim3(threads), lds, stream, static_cast<const char*>(a.X),
+                       static_cast<const char*>(a.codes), a.Y, a.plan, a.rows, a.groups, a.N, a.K, a.n_tiles, a.share, a.share_reciprocal);
     return check_launch();
 }
 
-template <int FMT, int G>
-int launch_many_g(const ManyArgs& a, bool swiglu, int64_t tiles, hipStream_t stream)
+template <int FMT, int G, bool GATED>
+int launch_many_shape(const ManyArgs& a, int64_t rows, int64_t groups, int shape, hipStream_t stream)
 {
-    return swiglu ? launch_many<FMT, G, true>(a, tiles, stream) : launch_many<FMT, G, false>(a, tiles, stream);
+    if (shape == 1) return launch_many<FMT, G, GATED, 2, 2, 4>(a, rows, groups, stream);
+    if (shape == 2) return launch_many<FMT, G, GATED, 4, 2, 2>(a, rows, groups, stream);
+    return launch_many<FMT, G, GATED, 4, 4, 1>(a, rows, groups, stream);
 }
 
 }  // namespace
 
-int launch_grouped_many(const GroupedArgs& g, int format, hipStream_t stream)
+int launch_grouped_many(const GroupedArgs& g, int format, int shape, hipStream_t stream)
 {
-    const GroupPlan plan = plan_view(g.plan, g.rows, g.groups);
     ManyArgs a;
-    a.X = static_cast<const char*>(g.X);
-    a.codes = static_cast<const uint4*>(g.codes);
-    a.tiles = plan.tiles[kTileHeights - 1];
-    a.tile_count = plan.tile_counts + kTileHeights - 1;
-    a.order = plan.order;
+    a.X = g.X;
+    a.codes = g.codes;
     a.Y = g.Y;
-    a.group_bytes = row_blocks(g.N) * grouped_row_block_bytes(g, format);
+    a.plan = g.plan;
+    a.rows = (int)g.rows;
+    a.groups = (int)g.groups;
     a.N = (uint32_t)g.N;
     a.K = (uint32_t)g.K;
+    a.n_tiles = 0;
     a.share = (uint32_t)g.share;
     a.share_reciprocal = small_reciprocal(g.share);
-    const int64_t columns = g.swiglu ? BN / 2 : BN, n_out = g.swiglu ? g.N / 2 : g.N;
-    a.n_tiles = (uint32_t)((n_out + columns - 1) / columns);
-    const int64_t tiles = most_tiles(g.rows, g.groups, BM);
-    if (format == kGroupedE8) return launch_many_g<kGroupedE8, 128>(a, g.swiglu, tiles, stream);
-    auto go = [&](auto fmt_c) -> int {
-        constexpr int FMT = decltype(fmt_c)::value;
-        switch (g.group) {
-            case 32: return launch_many_g<FMT, 32>(a, g.swiglu, tiles, stream);
-            case 64: return launch_many_g<FMT, 64>(a, g.swiglu, tiles, stream);
-            default: return launch_many_g<FMT, 128>(a, g.swiglu, tiles, stream);
-        }
+    auto go = [&](auto fmt_c, auto g_c) -> int {
+        constexpr int FMT = decltype(fmt_c)::value, G = decltype(g_c)::value;
+        return g.swiglu ? launch_many_shape<FMT, G, true>(a, g.rows, g.groups, shape, stream) : launch_many_shape<FMT, G, false>(a, g.rows, g.groups, shape, stream);
     };
-    return format == kGroupedBf16 ? go(std::integral_constant<int, kGroupedBf16>{}) : go(std::integral_constant<int, kGroupedFp16>{});
+    using G32 = std::integral_constant<int, 32>;
+    using G64 = std::integral_constant<int, 64>;
+    using G128 = std::integral_constant<int, 128>;
+    if (format == kGroupedE8) return go(std::integral_constant<int, kGroupedE8>{}, G128{});
+    auto go_g = [&](auto fmt_c) -> int { return g.group == 32 ? go(fmt_c, G32{}) : g.group == 64 ? go(fmt_c, G64{}) : go(fmt_c, G128{}); };
+    return format == kGroupedBf16 ? go_g(std::integral_constant<int, kGroupedBf16>{}) : go_g(std::integral_constant<int, kGroupedFp16>{});
 }
 
 }  // namespace e0m4

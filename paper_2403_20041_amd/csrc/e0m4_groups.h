@@ -13,44 +13,48 @@ constexpr int kMaxChoices = 16;                 // experts of a token
 constexpr int kMaxShare = 255;                  // entries per row of X
 
 // Tiles: rows of one group, so many at most.  A kernel has a workgroup (or several) for every tile of the height that it was built for;
-// how many there are only the device knows, so it is launched for as many as there can be.
+// how many there are only the device knows, so it is launched for as many as there can be.  Tiles of 128 rows are listed by classes, those of
+// more than 96, 64, 32 rows and the others, each by groups: long work comes first, and every XCD gets its share of each.
 constexpr int kTileHeights = 4;
-constexpr int tile_height(int i) { return 16 << i; }    // 16, 32, 64, 128
-inline int64_t most_tiles(int64_t rows, int64_t groups, int height) { return rows / height + (groups < rows ? groups : rows); }
+constexpr int kTileClasses = 4;
+__host__ __device__ constexpr int tile_height(int i) { return 16 << i; }    // 16, 32, 64, 128
+__host__ __device__ inline int64_t most_tiles(int64_t rows, int64_t groups, int height) { return rows / height + (groups < rows ? groups : rows); }
 
 struct GroupTile {
     int group;
-    int first_tile;                             // of the group, in this list
-    int begin, end;                             // its rows: positions in the layout
+    int first_tile;                             // of the group, in this list (and class)
+    int begin, end;                             // the rows of these tiles: positions in the layout
 };
 
 // Layout in memory, in 32-bit words: offsets [groups + 1], order [rows] and place [rows], each padded to a multiple of four words, then
-// the number of tiles of each height, the lists of tiles, and the counts of the first launch's workgroups.
-constexpr int64_t round4(int64_t n) { return (n + 3) & ~(int64_t)3; }
+// where the classes of each height end in its list (heights below 128: one class), the lists of tiles, and the counts of the first
+// launch's workgroups.  Kernels are given its beginning and find the rest themselves: arguments that fit the registers that a launch fills (14 to 16 of
+// them) are there at once, others cost a load from memory each time that they are first used, 6 us of a kernel of 15.
+__host__ __device__ constexpr int64_t round4(int64_t n) { return (n + 3) & ~(int64_t)3; }
 constexpr int64_t kMaxCountBlocks = 256;
 struct GroupPlan {
     int* offsets;
     int* order;
     int* place;
-    int* tile_counts;
+    int* class_ends[kTileHeights];              // [kTileClasses]
     GroupTile* tiles[kTileHeights];
     int* counts;                                // [workgroups][groups + 1]
 };
 inline int64_t plan_words(int64_t rows, int64_t groups)
 {
-    int64_t n = round4(groups + 1) + 2 * round4(rows) + 4;
+    int64_t n = round4(groups + 1) + 2 * round4(rows) + kTileHeights * kTileClasses;
     for (int i = 0; i < kTileHeights; ++i) n += 4 * most_tiles(rows, groups, tile_height(i));
     return n + kMaxCountBlocks * round4(groups + 1);
 }
-inline GroupPlan plan_view(const void* plan, int64_t rows, int64_t groups)
+__host__ __device__ inline GroupPlan plan_view(const void* plan, int64_t rows, int64_t groups)
 {
     int* w = static_cast<int*>(const_cast<void*>(plan));
     GroupPlan p;
     p.offsets = w;
     p.order = p.offsets + round4(groups + 1);
     p.place = p.order + round4(rows);
-    p.tile_counts = p.place + round4(rows);
-    int* at = p.tile_counts + 4;
+    int* at = p.place + round4(rows);
+    for (int i = 0; i < kTileHeights; ++i, at += kTileClasses) p.class_ends[i] = at;
     for (int i = 0; i < kTileHeights; ++i) {
         p.tiles[i] = reinterpret_cast<GroupTile*>(at);
         at += 4 * most_tiles(rows, groups, tile_height(i));
@@ -93,7 +97,7 @@ struct GroupedArgs {
 enum { kGroupedFp16 = 0, kGroupedE8 = 1, kGroupedBf16 = 2 };
 int64_t grouped_row_block_bytes(const GroupedArgs& a, int format);
 int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t stream);      // tiles of 16, 32 or 64 rows
-int launch_grouped_many(const GroupedArgs& a, int format, hipStream_t stream);                 // tiles of 128 rows
+int launch_grouped_many(const GroupedArgs& a, int format, int shape, hipStream_t stream);
 
 // Low-rank adapters of rows (see e0m4.h).
 struct LoraArgs {

@@ -8,7 +8,7 @@
 //
 // Layout: a stable counting sort.  The entries of a group keep their order, so results depend on nothing but the choice: counts are
 // integers, an entry's rank among its like within a wavefront comes from ballots over the bits of its group, and wavefronts and workgroups
-// count in order.  Few entries are one workgroup's work (choice, counts, places and tiles in one launch); otherwise a first launch
+// count in order.  Up to 1024 entries are one workgroup's work (choice, counts, places and tiles in one launch); otherwise a first launch
 // chooses and counts per workgroup, and every workgroup of a second one adds up the counts before its own.
 // What bounds it: launches, and the chains of a few hundred dependent instructions in each.
 #include "e0m4_groups.h"
@@ -19,12 +19,11 @@ namespace e0m4 {
 
 namespace {
 
-constexpr int kWg = 1024;
-constexpr int kWaves = kWg / 64;
-// Entries of a call that one workgroup takes
-constexpr int64_t kOneWorkgroup = 2048;
+constexpr int kWg = 1024;                       // threads of a workgroup that lays entries out
+constexpr int kSmallWg = 256;                   // ... of few tokens by few experts: its barriers are cheaper
+constexpr int kSmallTokens = 32;
+constexpr int kCountThreads = 512;
 constexpr int kCountEntries = 256;              // entries of a workgroup of the first of two launches, at least
-constexpr int kCountThreads = 256;
 
 template <int LANES>
 __device__ inline float lanes_max(float v)
@@ -72,15 +71,21 @@ __device__ inline float lanes_sum(float v)
     return v;
 }
 
+// (as kernel arguments one by one, in registers from the start)
 struct Route {
     const void* logits;
-    int64_t tokens, logits_ld;
-    int dtype, groups, k, sigmoid, renormalise;
-    float factor;
-    const int* count;
     int* experts;
     float* weights;
+    const int* count;
+    int64_t logits_ld;
+    int tokens, groups;
+    float factor;
+    int dtype, k, sigmoid, renormalise;
 };
+#define ROUTE_PARAMETERS const void *logits, int *experts, float *weights, void *plan, const int *count, int64_t logits_ld, int tokens, int groups, float factor, uint32_t kind
+#define ROUTE_ARGUMENTS a.logits, a.experts, a.weights, plan, a.count, a.logits_ld, (int)a.tokens, a.groups, a.factor, \
+                        (uint32_t)(a.dtype | a.sigmoid << 2 | a.renormalise << 3 | a.k << 4)
+#define ROUTE Route{logits, experts, weights, count, logits_ld, tokens, groups, factor, (int)(kind & 3), (int)(kind >> 4), (int)(kind >> 2 & 1), (int)(kind >> 3 & 1)}
 
 __device__ inline float logit_at(const Route& a, int64_t at)
 {
@@ -148,9 +153,9 @@ __device__ inline void choose(const Route& a, int64_t token, int lane, int& expe
     weight *= a.factor;
 }
 
-// Experts and weights of tokens first ... last - 1 by a workgroup of THREADS.
+// Experts and weights of tokens first ... last - 1 by a workgroup of THREADS; `kept` gets the experts too.
 template <int THREADS, int LANES, int PER>
-__device__ inline void choose_tokens(const Route& a, int64_t first, int64_t last)
+__device__ inline void choose_tokens(const Route& a, int64_t first, int64_t last, int* kept)
 {
     const int lane = threadIdx.x % LANES;
     const int64_t there = a.count ? (int64_t)min(max(a.count[0], 0), 0x7fffffff) : a.tokens;
@@ -161,40 +166,58 @@ __device__ inline void choose_tokens(const Route& a, int64_t first, int64_t last
         float weight;
         choose<LANES, PER>(a, token < last ? token : last - 1, lane, expert, weight);
         if (token < last && lane < a.k) {
-            a.experts[token * a.k + lane] = token < there ? expert : -1;
+            const int chosen = token < there ? expert : -1;
+            a.experts[token * a.k + lane] = chosen;
             a.weights[token * a.k + lane] = token < there ? weight : 0.f;
+            kept[(token - first) * a.k + lane] = chosen;
         }
     }
 }
 
 __device__ inline int group_of(int index, int groups) { return (unsigned)index < (unsigned)groups ? index : groups; }
 
-// Running sums over the workgroup's threads of five numbers each; before[i] is the sum over the threads before this one, total[i] over all.
-struct Five {
-    int v[1 + kTileHeights];
+// Numbers of a group that are summed up over the groups before it: rows, tiles of 16, 32 and 64 rows, tiles of 128 rows by class.
+constexpr int kSums = 1 + (kTileHeights - 1) + kTileClasses;
+struct Sums {
+    int v[kSums];
 };
-__device__ inline Five scan_five(const Five& mine, Five (&waves)[kWaves])
+template <int CTRL, int ROWS>
+__device__ inline int shifted(int v)                    // another lane's v, 0 where there is none
+{
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+// Sums over the threads before this one, and over the first `threads`.
+template <int WAVES>
+__device__ inline void scan(const Sums& mine, Sums& before, Sums& all, Sums (&waves)[WAVES], int threads)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Five s = mine;
+    Sums s = mine;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-#pragma unroll
-        for (int i = 0; i < 1 + kTileHeights; ++i) {
-            const int o = __shfl_up(s.v[i], d);
-            if (lane >= d) s.v[i] += o;
-        }
+    for (int i = 0; i < kSums; ++i) {                   // within rows of 16 lanes, then over the rows
+        int v = s.v[i];
+        v += shifted<0x111, 0xF>(v);
+        v += shifted<0x112, 0xF>(v);
+        v += shifted<0x114, 0xF>(v);
+        v += shifted<0x118, 0xF>(v);
+        v += shifted<0x142, 0xA>(v);
+        v += shifted<0x143, 0xC>(v);
+        s.v[i] = v;
     }
     if (lane == 63) waves[wave] = s;
     __syncthreads();
-    Five before = s;
 #pragma unroll
-    for (int i = 0; i < 1 + kTileHeights; ++i) before.v[i] -= mine.v[i];
-    for (int w = 0; w < wave; ++w) {
-#pragma unroll
-        for (int i = 0; i < 1 + kTileHeights; ++i) before.v[i] += waves[w].v[i];
+    for (int i = 0; i < kSums; ++i) {
+        before.v[i] = s.v[i] - mine.v[i];
+        all.v[i] = 0;
     }
-    return before;
+    for (int w = 0; w * 64 < threads; ++w) {
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) {
+            const int n = waves[w].v[i];
+            if (w < wave) before.v[i] += n;
+            all.v[i] += n;
+        }
+    }
 }
 
 struct Layout {
@@ -204,192 +227,254 @@ struct Layout {
     int groups;
     int bits;                                   // of a group's number, that of `groups` itself included
 };
+__device__ inline Layout make_layout(const void* plan, const int* index, int rows, int groups)
+{
+    return Layout{plan_view(plan, rows, groups), rows, index, groups, 32 - __builtin_clz((unsigned)groups)};
+}
 
-// LDS of the layout's workgroups
-struct LayoutLds {
-    int next[kMaxGroups + 1];                   // where the next entry of a group goes
-    int first[1 + kTileHeights][kMaxGroups + 1];// where groups (and their tiles of each height) begin
-    uint16_t chunk[kWaves][kMaxGroups + 1];     // entries of a group in a wavefront's 64
-    Five waves[kWaves];
-};
-
-// Offsets and tile lists, part `part` of `parts` (rows of a group: `total` of thread g), and next[g] = begin of g + before.
-__device__ inline void lay_out_groups(const Layout& a, LayoutLds& lds, int total, int before, int part, int parts)
+// Offsets and tile lists, part `part` of `parts`; thread g has group g (`total` rows), the one behind the last those of none.  Where its entries begin.
+template <int WAVES>
+__device__ inline int lay_out_groups(const Layout& a, int total, int part, int parts, Sums (&waves)[WAVES])
 {
     const int g = threadIdx.x;
-    Five mine = {};
-    if (g <= a.groups) {
-        mine.v[0] = total;
+    Sums mine = {}, before, all;
+    const int last = total % tile_height(kTileHeights - 1), whole = total / tile_height(kTileHeights - 1);
+    const int last_class = last == 0 ? -1 : last > 96 ? 0 : last > 64 ? 1 : last > 32 ? 2 : 3;
+    if (g <= a.groups) mine.v[0] = total;
+    if (g < a.groups) {
 #pragma unroll
-        for (int i = 0; i < kTileHeights; ++i) mine.v[1 + i] = g < a.groups ? (total + tile_height(i) - 1) / tile_height(i) : 0;
+        for (int i = 0; i < kTileHeights - 1; ++i) mine.v[1 + i] = (total + tile_height(i) - 1) / tile_height(i);
+        mine.v[kTileHeights] = whole + (last_class == 0 ? 1 : 0);
+#pragma unroll
+        for (int c = 1; c < kTileClasses; ++c) mine.v[kTileHeights + c] = last_class == c ? 1 : 0;
     }
-    const Five begin = scan_five(mine, lds.waves);
-    if (g <= a.groups) {
-        lds.next[g] = begin.v[0] + before;
-#pragma unroll
-        for (int i = 0; i < 1 + kTileHeights; ++i) lds.first[i][g] = begin.v[i];
-        if (part == 0) {
-            a.plan.offsets[g] = begin.v[0];
-            if (g == a.groups) {
-#pragma unroll
-                for (int i = 0; i < kTileHeights; ++i) a.plan.tile_counts[i] = begin.v[1 + i];
-            }
-        }
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < kTileHeights; ++i) {
-        const int* first = lds.first[1 + i];
-        const int tiles = first[a.groups];
-        for (int t = part * kWg + threadIdx.x; t < tiles; t += parts * kWg) {
-            int lo = 0, hi = a.groups;          // the last group that begins at or before t
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (first[mid] <= t) lo = mid;
-                else hi = mid;
-            }
-            // (of groups that begin at the same tile all but the last are empty)
-            a.plan.tiles[i][t] = GroupTile{lo, first[lo], lds.first[0][lo], lds.first[0][lo + 1]};
-        }
-    }
-}
-
-// Entries first ... last - 1 to their places, 1024 at a time.
-__device__ inline void place_entries(const Layout& a, LayoutLds& lds, int64_t first, int64_t last)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t base = first; base < last; base += kWg) {
-        if ((int)threadIdx.x <= a.groups) {
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) lds.chunk[w][threadIdx.x] = 0;
-        }
-        __syncthreads();
-        const int64_t entry = base + threadIdx.x;
-        const bool in = entry < last;
-        const int g = in ? group_of(a.index[entry], a.groups) : 0;
-        uint64_t like = __ballot(in);
-        for (int b = 0; b < a.bits; ++b) {
-            const uint64_t set = __ballot((g >> b) & 1);
-            like &= ((g >> b) & 1) ? set : ~set;
-        }
-        const int rank = __popcll(like & (((uint64_t)1 << lane) - 1));
-        if (in && rank == 0) lds.chunk[wave][g] = (uint16_t)__popcll(like);
-        __syncthreads();
-        if ((int)threadIdx.x <= a.groups) {     // counts of the wavefronts before
+    scan(mine, before, all, waves, a.groups + 1);
+    const int begin = before.v[0], end = begin + total;
+    if (g <= a.groups && part == 0) {
+        a.plan.offsets[g] = begin;
+        if (g == a.groups) {
             int sum = 0;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const int n = lds.chunk[w][threadIdx.x];
-                lds.chunk[w][threadIdx.x] = (uint16_t)sum;
-                sum += n;
+            for (int i = 0; i < kTileHeights - 1; ++i) {
+#pragma unroll
+                for (int c = 0; c < kTileClasses; ++c) a.plan.class_ends[i][c] = all.v[1 + i];
             }
-            lds.first[0][threadIdx.x] = sum;    // (the groups' begins are not needed any more)
+#pragma unroll
+            for (int c = 0; c < kTileClasses; ++c) {
+                sum += all.v[kTileHeights + c];
+                a.plan.class_ends[kTileHeights - 1][c] = sum;
+            }
         }
-        __syncthreads();
-        if (in) {
-            const int to = lds.next[g] + lds.chunk[wave][g] + rank;
-            a.plan.order[to] = (int)entry;
-            a.plan.place[entry] = g < a.groups ? to : -1;
-        }
-        __syncthreads();
-        if ((int)threadIdx.x <= a.groups) lds.next[threadIdx.x] += lds.first[0][threadIdx.x];
     }
+    if (g < a.groups) {
+#pragma unroll
+        for (int i = 0; i < kTileHeights - 1; ++i) {
+            for (int t = part; t < mine.v[1 + i]; t += parts) a.plan.tiles[i][before.v[1 + i] + t] = GroupTile{g, before.v[1 + i], begin, end};
+        }
+        GroupTile* tiles = a.plan.tiles[kTileHeights - 1];
+        const int whole_end = last_class == 0 ? end : begin + whole * tile_height(kTileHeights - 1);
+        for (int t = part; t < mine.v[kTileHeights]; t += parts)
+            tiles[before.v[kTileHeights] + t] = GroupTile{g, before.v[kTileHeights], begin, whole_end};
+        int of_class = all.v[kTileHeights];             // where the class begins
+#pragma unroll
+        for (int c = 1; c < kTileClasses; ++c) {
+            if (last_class == c && part == 0) tiles[of_class + before.v[kTileHeights + c]] = GroupTile{g, of_class + before.v[kTileHeights + c], whole_end, end};
+            of_class += all.v[kTileHeights + c];
+        }
+    }
+    return begin;
 }
 
-// Few entries: everything in one workgroup.
-template <int LANES, int PER, bool CHOOSE>
-__global__ __launch_bounds__(kWg) void route_small_kernel(Route r, Layout a)
+// Rank of an entry among those of its group in its wavefront, and how many there are.
+__device__ inline int rank_among_like(int g, bool in, int bits, int& like_in_wave)
 {
-    __shared__ LayoutLds lds;
-    int* count = lds.first[1];                  // (read by the thread of its group before begins come there)
-    if ((int)threadIdx.x <= a.groups) count[threadIdx.x] = 0;
-    if constexpr (CHOOSE) choose_tokens<kWg, LANES, PER>(r, 0, r.tokens);
-    __syncthreads();                            // (the choice is read back by other threads of the workgroup: the barrier waits for the stores)
-    for (int64_t i = threadIdx.x; i < a.rows; i += kWg) atomicAdd(&count[group_of(a.index[i], a.groups)], 1);
+    uint64_t like = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((g >> b) & 1);
+        like &= ((g >> b) & 1) ? set : ~set;
+    }
+    like_in_wave = __popcll(like);
+    return __popcll(like & (((uint64_t)1 << (threadIdx.x & 63)) - 1));
+}
+
+template <int THREADS>
+struct LayoutLds {
+    int next[THREADS];                          // where the next entry of a group goes
+    uint16_t chunk[THREADS / 64][THREADS];      // entries of a group in a wavefront's 64, then in those of the wavefronts before
+    Sums waves[THREADS / 64];
+};
+template <int THREADS>
+__device__ inline void clear_chunks(LayoutLds<THREADS>& lds, int groups)
+{
+    if ((int)threadIdx.x <= groups) {
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) lds.chunk[w][threadIdx.x] = 0;
+    }
+}
+// Thread g: chunk[w][g] becomes the sum over the wavefronts before w; the sum over all.
+template <int THREADS>
+__device__ inline int sum_chunks(LayoutLds<THREADS>& lds, int groups)
+{
+    int sum = 0;
+    if ((int)threadIdx.x <= groups) {
+        int n[THREADS / 64];
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) n[w] = lds.chunk[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            lds.chunk[w][threadIdx.x] = (uint16_t)sum;
+            sum += n[w];
+        }
+    }
+    return sum;
+}
+
+// Few entries, one to a thread at most, and groups, one to a thread with the one behind the last: everything in one workgroup.
+template <int THREADS, int LANES, int PER, bool CHOOSE>
+__global__ __launch_bounds__(THREADS) void route_small_kernel(ROUTE_PARAMETERS)
+{
+    const Route r = ROUTE;
+    const Layout a = make_layout(plan, experts, tokens * r.k, groups);
+    __shared__ LayoutLds<THREADS> lds;
+    __shared__ int kept[THREADS];
+    clear_chunks(lds, a.groups);
+    const int t = threadIdx.x;
+    const bool in = t < (int)a.rows;
+    if constexpr (CHOOSE) choose_tokens<THREADS, LANES, PER>(r, 0, r.tokens, kept);
     __syncthreads();
-    lay_out_groups(a, lds, (int)threadIdx.x <= a.groups ? count[threadIdx.x] : 0, 0, 0, 1);
+    const int g = in ? group_of(CHOOSE ? kept[t] : a.index[t], a.groups) : 0;
+    int like;
+    const int rank = rank_among_like(g, in, a.bits, like);
+    if (in && rank == 0) lds.chunk[t >> 6][g] = (uint16_t)like;
     __syncthreads();
-    place_entries(a, lds, 0, a.rows);
+    const int total = sum_chunks(lds, a.groups);
+    lds.next[t] = lay_out_groups(a, total, 0, 1, lds.waves);
+    __syncthreads();
+    if (in) {
+        const int to = lds.next[g] + lds.chunk[t >> 6][g] + rank;
+        a.plan.order[to] = t;
+        a.plan.place[t] = g < a.groups ? to : -1;
+    }
 }
 
 // Many entries, first launch: the choice, and counts of the workgroup's entries.
 template <int LANES, int PER, bool CHOOSE>
-__global__ __launch_bounds__(kCountThreads) void route_count_kernel(Route r, Layout a, int64_t tokens_each)
+__global__ __launch_bounds__(kCountThreads) void route_count_kernel(ROUTE_PARAMETERS, int tokens_each)
 {
-    __shared__ int count[kMaxGroups + 1];
-    for (int i = threadIdx.x; i <= a.groups; i += kCountThreads) count[i] = 0;
-    const int64_t first = (int64_t)blockIdx.x * tokens_each, last = min(first + tokens_each, r.tokens);
-    if constexpr (CHOOSE) choose_tokens<kCountThreads, LANES, PER>(r, first, last);
-    if (a.plan.offsets == nullptr) return;      // (no layout is wanted)
+    const Route r = ROUTE;
+    const Layout a = make_layout(plan, experts, tokens * r.k, groups);
+    __shared__ int counted[kMaxGroups + 1];
+    __shared__ int kept[kCountThreads / LANES * kMaxChoices];
+    for (int i = threadIdx.x; i <= a.groups; i += kCountThreads) counted[i] = 0;
+    const int64_t first = (int64_t)blockIdx.x * tokens_each, last = min(first + tokens_each, (int64_t)r.tokens);
     __syncthreads();
-    for (int64_t i = first * r.k + threadIdx.x; i < last * r.k; i += kCountThreads) atomicAdd(&count[group_of(a.index[i], a.groups)], 1);
-    __syncthreads();
-    for (int i = threadIdx.x; i <= a.groups; i += kCountThreads) a.plan.counts[(int64_t)blockIdx.x * (a.groups + 1) + i] = count[i];
+    if constexpr (CHOOSE) {
+        // (as many tokens at a time as the workgroup has lanes for)
+        for (int64_t at = first; at < last; at += kCountThreads / LANES) {
+            const int64_t to = min(at + kCountThreads / LANES, last);
+            choose_tokens<kCountThreads, LANES, PER>(r, at, to, kept);
+            if (plan == nullptr) continue;    // (no layout is wanted)
+            __syncthreads();
+            for (int i = threadIdx.x; i < (int)(to - at) * r.k; i += kCountThreads) atomicAdd(&counted[group_of(kept[i], a.groups)], 1);
+            __syncthreads();
+        }
+    } else {
+        for (int64_t i = first + threadIdx.x; i < last; i += kCountThreads) atomicAdd(&counted[group_of(a.index[i], a.groups)], 1);
+        __syncthreads();
+    }
+    if (plan == nullptr) return;
+    for (int i = threadIdx.x; i <= a.groups; i += kCountThreads) a.plan.counts[(int64_t)blockIdx.x * (a.groups + 1) + i] = counted[i];
 }
 
 // ... second launch: workgroup p places the entries that workgroups p * each ... of the first counted.
-__global__ __launch_bounds__(kWg) void route_place_kernel(Layout a, int blocks, int each, int64_t entries_each)
+__global__ __launch_bounds__(kWg) void route_place_kernel(const int* index, void* plan, int rows, int groups, int blocks, int each, int64_t entries_each)
 {
-    __shared__ LayoutLds lds;
-    int *total = lds.first[1], *before = lds.first[2];     // (read by the thread of their group before begins come there)
-    const int n = a.groups + 1;
-    if ((int)threadIdx.x < n) total[threadIdx.x] = before[threadIdx.x] = 0;
+    const Layout a = make_layout(plan, index, rows, groups);
+    __shared__ LayoutLds<kWg> lds;
+    __shared__ int total[kWg], before[kWg];
+    const int n = a.groups + 1, t = threadIdx.x;
+    if (t < n) total[t] = before[t] = 0;
     __syncthreads();
     // Thread (part, g) adds up every parts-th workgroup's count of g.
-    const int parts = kWg / n, g = threadIdx.x % n, part = threadIdx.x / n, mine = blockIdx.x * each;
+    const int parts = kWg / n, g_mine = t % n, part = t / n, mine = blockIdx.x * each;
     if (part < parts) {
         int sum = 0, early = 0;
-        for (int b = part; b < blocks; b += parts) {
-            const int c = a.plan.counts[(int64_t)b * n + g];
-            sum += c;
-            early += b < mine ? c : 0;
+        const int* counts = a.plan.counts + g_mine;
+        for (int b = part; b < blocks; b += parts * 8) {
+            int c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = b + i * parts < blocks ? counts[(b + i * parts) * n] : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum += c[i];
+                early += b + i * parts < mine ? c[i] : 0;
+            }
         }
-        atomicAdd(&total[g], sum);
-        atomicAdd(&before[g], early);
+        atomicAdd(&total[g_mine], sum);
+        atomicAdd(&before[g_mine], early);
     }
     __syncthreads();
-    const bool in = (int)threadIdx.x < n;
-    lay_out_groups(a, lds, in ? total[threadIdx.x] : 0, in ? before[threadIdx.x] : 0, blockIdx.x, gridDim.x);
-    __syncthreads();
-    place_entries(a, lds, mine * entries_each, min((int64_t)(mine + each) * entries_each, a.rows));
+    const int begin = lay_out_groups(a, t < n ? total[t] : 0, blockIdx.x, gridDim.x, lds.waves);
+    lds.next[t] = begin + (t < n ? before[t] : 0);
+    // 1024 entries at a time
+    const int64_t first = mine * entries_each, last = min((int64_t)(mine + each) * entries_each, a.rows);
+    for (int64_t base = first; base < last; base += kWg) {
+        clear_chunks(lds, a.groups);
+        __syncthreads();
+        const int64_t entry = base + t;
+        const bool in = entry < last;
+        const int g = in ? group_of(a.index[entry], a.groups) : 0;
+        int like;
+        const int rank = rank_among_like(g, in, a.bits, like);
+        if (in && rank == 0) lds.chunk[t >> 6][g] = (uint16_t)like;
+        __syncthreads();
+        const int sum = sum_chunks(lds, a.groups);
+        __syncthreads();
+        if (in) {
+            const int to = lds.next[g] + lds.chunk[t >> 6][g] + rank;
+            a.plan.order[to] = (int)entry;
+            a.plan.place[entry] = g < a.groups ? to : -1;
+        }
+        __syncthreads();
+        if (t <= a.groups) lds.next[t] += sum;
+    }
 }
 
 template <int LANES, int PER, bool CHOOSE>
-int launch_route_as(const Route& r, const Layout& a, hipStream_t stream)
+int launch_route_as(const RouteArgs& a, void* plan, hipStream_t stream)
 {
-    if (a.plan.offsets && a.rows <= kOneWorkgroup) {
-        hipLaunchKernelGGL((route_small_kernel<LANES, PER, CHOOSE>), dim3(1), dim3(kWg), 0, stream, r, a);
+    const int64_t rows = a.tokens * a.k;
+    if (plan && rows <= kSmallWg && a.tokens <= (CHOOSE ? kSmallTokens : kSmallWg) && a.groups < kSmallWg) {
+        hipLaunchKernelGGL((route_small_kernel<kSmallWg, LANES, PER, CHOOSE>), dim3(1), dim3(kSmallWg), 0, stream, ROUTE_ARGUMENTS);
         return check_launch();
     }
-    int64_t each = (kCountEntries + r.k - 1) / r.k;
-    if (each * kMaxCountBlocks < r.tokens) each = (r.tokens + kMaxCountBlocks - 1) / kMaxCountBlocks;
-    const int blocks = (int)((r.tokens + each - 1) / each);
-    hipLaunchKernelGGL((route_count_kernel<LANES, PER, CHOOSE>), dim3((unsigned)blocks), dim3(kCountThreads), 0, stream, r, a, each);
+    if (plan && rows <= kWg) {
+        hipLaunchKernelGGL((route_small_kernel<kWg, LANES, PER, CHOOSE>), dim3(1), dim3(kWg), 0, stream, ROUTE_ARGUMENTS);
+        return check_launch();
+    }
+    int64_t each = (kCountEntries + a.k - 1) / a.k;
+    if (each * kMaxCountBlocks < a.tokens) each = (a.tokens + kMaxCountBlocks - 1) / kMaxCountBlocks;
+    const int blocks = (int)((a.tokens + each - 1) / each);
+    const int together = each * a.k < kWg ? (int)(kWg / (each * a.k)) : 1;
+    if (blocks == 0) return E0M4_OK;
+    hipLaunchKernelGGL((route_count_kernel<LANES, PER, CHOOSE>), dim3((unsigned)blocks), dim3(kCountThreads), 0, stream, ROUTE_ARGUMENTS, (int)each);
     const int rc = check_launch();
-    if (rc != E0M4_OK || !a.plan.offsets) return rc;
-    const int together = each * r.k < kWg ? (int)(kWg / (each * r.k)) : 1;
-    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)((blocks + together - 1) / together)), dim3(kWg), 0, stream, a, blocks, together, each * r.k);
+    if (rc != E0M4_OK || !plan) return rc;
+    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)((blocks + together - 1) / together)), dim3(kWg), 0, stream, a.experts, plan, (int)rows, a.groups,
+                       blocks, together, each * a.k);
     return check_launch();
 }
 
 }  // namespace
 
-int launch_route(const RouteArgs& args, void* plan, hipStream_t stream)
+int launch_route(const RouteArgs& a, void* plan, hipStream_t stream)
 {
-    const Route r{args.logits, args.tokens, args.logits_ld, args.dtype, args.groups, args.k, args.sigmoid, args.renormalise, args.factor, args.count, args.experts,
-                  args.weights};
-    Layout a = {};
-    a.rows = args.tokens * args.k;
-    if (plan) a.plan = plan_view(plan, a.rows, args.groups);
-    a.index = args.experts;
-    a.groups = args.groups;
-    while ((1 << a.bits) <= args.groups) ++a.bits;
-    if (!args.logits) return launch_route_as<16, 1, false>(r, a, stream);
-    if (args.groups <= 16) return launch_route_as<16, 1, true>(r, a, stream);
-    if (args.groups <= 64) return launch_route_as<16, 4, true>(r, a, stream);
-    if (args.groups <= 128) return launch_route_as<16, 8, true>(r, a, stream);
-    if (args.groups <= 256) return launch_route_as<16, 16, true>(r, a, stream);
-    return launch_route_as<64, 16, true>(r, a, stream);
+    if (!a.logits) return launch_route_as<16, 1, false>(a, plan, stream);
+    if (a.groups <= 16) return launch_route_as<16, 1, true>(a, plan, stream);
+    if (a.groups <= 64) return launch_route_as<16, 4, true>(a, plan, stream);
+    if (a.groups <= 128) return launch_route_as<16, 8, true>(a, plan, stream);
+    if (a.groups <= 256) return launch_route_as<16, 16, true>(a, plan, stream);
+    return launch_route_as<64, 16, true>(a, plan, stream);
 }
 
 // ---- weighted sum of a token's rows ----------------------------------------------------------------------------------

@@ -69,7 +69,7 @@ int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows,
     a.Y = Y;
     const int force = knob(Knob::grouped_tile);
     const int height = force == 16 || force == 32 || force == 64 || force == 128 ? force : grouped_height(rows, groups);
-    return height == 128 ? launch_grouped_many(a, format, (hipStream_t)stream) : launch_grouped_few(a, format, height, (hipStream_t)stream);
+    return height == 128 ? launch_grouped_many(a, format, knob(Knob::grouped_exact), (hipStream_t)stream) : launch_grouped_few(a, format, height, (hipStream_t)stream);
 }
 
 int check_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
@@ -81,8 +81,6 @@ int check_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
 }
 
 }  // namespace
-
-int64_t grouped_row_block_bytes(const GroupedArgs& a, int format) { return row_block_bytes(a.K, a.group, format); }
 
 }  // namespace e0m4
 

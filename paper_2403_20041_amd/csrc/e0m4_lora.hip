@@ -323,7 +323,7 @@ int launch_lora(const LoraArgs& l, void* workspace, hipStream_t stream)
     a.X = static_cast<const char*>(l.X);
     a.x_ld = (uint32_t)(l.x_ld * 2);
     a.tiles = plan.tiles[p.height_index];
-    a.tile_count = plan.tile_counts + p.height_index;
+    a.tile_count = plan.class_ends[p.height_index] + kTileClasses - 1;
     a.offsets = plan.offsets;
     a.order = plan.order;
     a.rows = l.rows;
