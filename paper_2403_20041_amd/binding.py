@@ -532,11 +532,13 @@ class E0M4Groups(NamedTuple):
 
     @property
     def order(self) -> torch.Tensor:
-        return self.data[(self.groups + 4) // 4 * 4:][:self.rows]
+        first = (self.groups + 4) // 4 * 4
+        return self.data[first:first + self.rows]
 
     @property
     def place(self) -> torch.Tensor:
-        return self.data[(self.groups + 4) // 4 * 4 + (self.rows + 3) // 4 * 4:][:self.rows]
+        first = (self.groups + 4) // 4 * 4 + (self.rows + 3) // 4 * 4
+        return self.data[first:first + self.rows]
 
 
 @functools.lru_cache(maxsize=1024)
@@ -591,11 +593,13 @@ def e0m4_route(logits: torch.Tensor, k: int, scoring: int = E0M4_ROUTE_SOFTMAX, 
     device = logits.device
     if plan is None:
         plan = e0m4_groups_alloc(tokens * k, experts, device, stream)
+        pointer = plan.data.data_ptr()
+    else:
+        pointer = _groups_plan(plan, tokens * k, experts, "e0m4_route")
     chosen = _empty((tokens, k), torch.int32, device, stream, "chosen")
     weights = _empty((tokens, k), torch.float32, device, stream, "weights")
     _check(lib().e0m4_route(logits.data_ptr(), _DTYPES[logits.dtype], tokens, experts, logits.stride(0), k, scoring, 1 if renormalise else 0, factor,
-                            _ptr(count), chosen.data_ptr(), weights.data_ptr(), _groups_plan(plan, tokens * k, experts, "e0m4_route"),
-                            _stream(stream)), "e0m4_route")
+                            _ptr(count), chosen.data_ptr(), weights.data_ptr(), pointer, _stream(stream)), "e0m4_route")
     return chosen, weights, plan
 
 
@@ -661,6 +665,7 @@ def _lora_rows(t, dtype, shape, name: str) -> int:
     return t.stride(0) if shape[0] > 1 else shape[1]
 
 
+@functools.lru_cache(maxsize=1024)
 def e0m4_lora_workspace_bytes(rows: int, adapters: int, rank: int, N: int, K: int) -> int:
     return lib().e0m4_lora_workspace_bytes(rows, adapters, rank, N, K)
 

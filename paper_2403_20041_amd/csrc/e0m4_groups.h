@@ -64,7 +64,7 @@ __host__ __device__ inline GroupPlan plan_view(const void* plan, int64_t rows, i
 }
 
 // x / d for x < 2^24, 1 <= d <= 255: the product with the rounded-up reciprocal is off by less than x / 2^32 < 1 / d.
-inline uint32_t small_reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0; }
+__host__ __device__ inline uint32_t small_reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0; }
 __device__ inline uint32_t small_quotient(uint32_t x, uint32_t reciprocal) { return reciprocal ? __umulhi(x, reciprocal) : x; }
 
 // The expert choice of a router, and the layout (see e0m4.h).  logits null: `experts` is read, one entry per token, and laid out.

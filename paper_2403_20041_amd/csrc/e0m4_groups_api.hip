@@ -77,7 +77,7 @@ int check_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
     const int rc = check_groups(rows, adapters);
     if (rc != E0M4_OK) return rc;
     if (rank < 8 || rank > 128 || rank % 8 != 0 || N < 0 || N > (int64_t)1 << 24 || N % 8 != 0 || K < 8 || K > (int64_t)1 << 20 || K % 8 != 0) return E0M4_ERR_SHAPE;
-    return E0M4_OK;
+    return N * rank * 2 > kMaxXBytes ? E0M4_ERR_SHAPE : E0M4_OK;     // (rows of one adapter's B are reached by 32-bit offsets)
 }
 
 }  // namespace

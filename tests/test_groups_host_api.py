@@ -95,7 +95,7 @@ def test_lora_refuses(L):
 
     for bad in (dict(dtype=2), dict(rows=-1), dict(adapters=0), dict(adapters=1024), dict(rank=0), dict(rank=12), dict(rank=136), dict(N=100), dict(N=-8),
                 dict(K=0), dict(K=252), dict(x_ld=248), dict(out_ld=120), dict(base=FAR, base_ld=120), dict(base=FAR, base_ld=136, out=FAR),
-                dict(rows=1 << 23, x_ld=256)):
+                dict(rows=1 << 23, x_ld=256), dict(rank=128, N=1 << 23, out_ld=1 << 23)):
         assert call(**bad) == SHAPE, bad
     for bad in (dict(X=None), dict(plan=None), dict(A=None), dict(B=None), dict(out=None), dict(ws=None)):
         assert call(**bad) == NULL, bad
