@@ -31,8 +31,7 @@ const char* const kKnobNames[] = {      // in the order of Knob
     "gemm_split_order",           // work items of a K-split launch: 1 by tile, 2 by split (0: by the length of a split)
     "kv4_attention",              // attention over a cache in 4 bits: 1 the kernel for few queries, 2 the one for many, 3 that with 256 rows to a workgroup
     "kv4_chunk",                  // ... tiles of the cache to a workgroup
-    "grouped_tile",               // grouped products: rows of a tile (16, 32, 64 or 128)
-    "grouped_exact",
+    "grouped_form",               // grouped products: the form of kGroupedForms, from 1 on
 };
 static_assert(sizeof(kKnobNames) / sizeof(kKnobNames[0]) == (size_t)Knob::count, "a name for each");
 

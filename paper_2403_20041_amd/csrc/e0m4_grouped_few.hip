@@ -1,5 +1,5 @@
-// Products of a layout's rows with the quantised weights of their groups, few rows to a group (e0m4_matmul_grouped and its like): tiles of 16, 32
-// or 64 rows of one group, the weight operand of the matrix cores made in registers from the packed codes.
+// Products of a layout's rows with the quantised weights of their groups, few rows to a group (e0m4_matmul_grouped and its like): tiles of 16 or 32
+// rows of one group, the weight operand of the matrix cores made in registers from the packed codes.
 //     Y[p, n] = sum_k X[row(p), k] * dequant(codes of p's group)[n, k], and with the gated product silu(gate) * up of the two halves of n.
 //
 // A workgroup has one tile and R consecutive row blocks (16 weight rows; R / 2 blocks of the gate and the same of the up projection); its four
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(const char*
     constexpr int PPR = NP * 4, RPI = 64 / PPR, RB = PPR * 16, XE = NP;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const GroupPlan lay = plan_view(plan, rows, groups);
-    constexpr int HEIGHT = MT == 1 ? 0 : MT == 2 ? 1 : 2;
+    constexpr int HEIGHT = MT - 1;
     static_assert(tile_height(HEIGHT) == 16 * MT, "a list of tiles");
     const uint32_t share = kind >> 4;
     const int group_shift = (int)(kind & 15);
@@ -290,20 +290,17 @@ int launch_few(const FewArgs& f, int64_t tiles, hipStream_t stream)
 }
 
 template <int FMT, bool GATED>
-int launch_few_as(const FewArgs& f, int64_t tiles, int height, hipStream_t stream)
+int launch_few_as(const FewArgs& f, int64_t tiles, int height, int row_blocks, hipStream_t stream)
 {
-    const int r = knob(Knob::grouped_exact);
-    switch (height) {
-        case 16: return r == 1 ? launch_few<FMT, 1, 2, GATED>(f, tiles, stream) : launch_few<FMT, 1, 4, GATED>(f, tiles, stream);
-        case 32: return r == 1 ? launch_few<FMT, 2, 2, GATED>(f, tiles, stream) : launch_few<FMT, 2, 4, GATED>(f, tiles, stream);
-        case 64: return r == 1 ? launch_few<FMT, 4, 4, GATED>(f, tiles, stream) : launch_few<FMT, 4, 2, GATED>(f, tiles, stream);
-        default: return E0M4_ERR_SHAPE;
-    }
+    if (height == 32 && row_blocks == 4) return launch_few<FMT, 2, 4, GATED>(f, tiles, stream);
+    if (height == 16 && row_blocks == 4) return launch_few<FMT, 1, 4, GATED>(f, tiles, stream);
+    if (height == 16 && row_blocks == 2) return launch_few<FMT, 1, 2, GATED>(f, tiles, stream);
+    return E0M4_ERR_SHAPE;
 }
 
 }  // namespace
 
-int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t stream)
+int launch_grouped_few(const GroupedArgs& a, int format, int height, int row_blocks, hipStream_t stream)
 {
     FewArgs f;
     f.X = a.X;
@@ -320,7 +317,8 @@ int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t
     const int64_t tiles = most_tiles(a.rows, a.groups, height);
     auto go = [&](auto fmt_c) -> int {
         constexpr int FMT = decltype(fmt_c)::value;
-        return a.swiglu ? launch_few_as<FMT, true>(f, tiles, height, stream) : launch_few_as<FMT, false>(f, tiles, height, stream);
+        return a.swiglu ? launch_few_as<FMT, true>(f, tiles, height, row_blocks, stream)
+                        : launch_few_as<FMT, false>(f, tiles, height, row_blocks, stream);
     };
     switch (format) {
         case kGroupedFp16: return go(std::integral_constant<int, kGroupedFp16>{});

@@ -442,16 +442,17 @@ int launch_many(const ManyArgs& f, int64_t rows, int64_t groups, hipStream_t str
 }
 
 template <int FMT, int G, bool GATED>
-int launch_many_shape(const ManyArgs& a, int64_t rows, int64_t groups, int shape, hipStream_t stream)
+int launch_many_shape(const ManyArgs& a, int64_t rows, int64_t groups, int height, int columns, hipStream_t stream)
 {
-    if (shape == 1) return launch_many<FMT, G, GATED, 2, 2, 4>(a, rows, groups, stream);
-    if (shape == 2) return launch_many<FMT, G, GATED, 4, 2, 2>(a, rows, groups, stream);
-    return launch_many<FMT, G, GATED, 4, 4, 1>(a, rows, groups, stream);
+    if (height == 128 && columns == 256) return launch_many<FMT, G, GATED, 4, 4, 1>(a, rows, groups, stream);
+    if (height == 128 && columns == 128) return launch_many<FMT, G, GATED, 4, 2, 2>(a, rows, groups, stream);
+    if (height == 64 && columns == 128) return launch_many<FMT, G, GATED, 2, 2, 4>(a, rows, groups, stream);
+    return E0M4_ERR_SHAPE;
 }
 
 }  // namespace
 
-int launch_grouped_many(const GroupedArgs& g, int format, int shape, hipStream_t stream)
+int launch_grouped_many(const GroupedArgs& g, int format, int height, int columns, hipStream_t stream)
 {
     ManyArgs a;
     a.X = g.X;
@@ -467,7 +468,8 @@ int launch_grouped_many(const GroupedArgs& g, int format, int shape, hipStream_t
     a.share_reciprocal = small_reciprocal(g.share);
     auto go = [&](auto fmt_c, auto g_c) -> int {
         constexpr int FMT = decltype(fmt_c)::value, G = decltype(g_c)::value;
-        return g.swiglu ? launch_many_shape<FMT, G, true>(a, g.rows, g.groups, shape, stream) : launch_many_shape<FMT, G, false>(a, g.rows, g.groups, shape, stream);
+        return g.swiglu ? launch_many_shape<FMT, G, true>(a, g.rows, g.groups, height, columns, stream)
+                        : launch_many_shape<FMT, G, false>(a, g.rows, g.groups, height, columns, stream);
     };
     using G32 = std::integral_constant<int, 32>;
     using G64 = std::integral_constant<int, 64>;

@@ -96,8 +96,8 @@ struct GroupedArgs {
 };
 enum { kGroupedFp16 = 0, kGroupedE8 = 1, kGroupedBf16 = 2 };
 int64_t grouped_row_block_bytes(const GroupedArgs& a, int format);
-int launch_grouped_few(const GroupedArgs& a, int format, int height, hipStream_t stream);      // tiles of 16, 32 or 64 rows
-int launch_grouped_many(const GroupedArgs& a, int format, int shape, hipStream_t stream);
+int launch_grouped_few(const GroupedArgs& a, int format, int height, int row_blocks, hipStream_t stream);     // tiles of 16 or 32 rows
+int launch_grouped_many(const GroupedArgs& a, int format, int height, int columns, hipStream_t stream);       // tiles of 64 or 128 rows
 
 // Low-rank adapters of rows (see e0m4.h).
 struct LoraArgs {

@@ -2,6 +2,8 @@
 // before anything is enqueued.
 #include "e0m4_groups.h"
 
+#include <math.h>
+
 namespace e0m4 {
 
 namespace {
@@ -40,11 +42,48 @@ int check_grouped(int64_t rows, int64_t groups, int64_t share, int64_t N, int64_
     return E0M4_OK;
 }
 
-// Tiles of the height nearest to the rows of a group.
-int grouped_height(int64_t rows, int64_t groups)
+// The forms of the product, and what an estimate of their launches' time goes by, in us: with w the workgroups for each of the 256 compute units, r rows of a
+// tile that exist on average and b k blocks of 128 that a part of a workgroup walks,
+//     start + b * max(one + one_row r, (full + full_row r) w) + each w,
+// b's factor times a format's own.  Workgroups are counted as if every row chose a group at random.
+// The constants are a least-squares fit (logarithm of the ratio to the measurement, rms 11 - 14 %) to 6277 problems, each timed in all forms: 4 to 128
+// groups, 1 to 250 rows to a group, gated and plain, 512 to 27392 columns, 512 to 14080 weights a row, all formats and groups.  Choosing by the
+// estimate costs 1.9 % over the best form of each (geometric mean); without one of the forms 2.2 - 2.5 %, without the second 6.0, without the
+// fourth 9.0.
+struct GroupedForm {
+    int height;                                         // rows of a tile
+    int columns;                                        // weight rows of a workgroup
+    int parts;                                          // of K, side by side
+    double start, one, one_row, full, full_row, each, bf16, e8;
+};
+constexpr GroupedForm kGroupedForms[] = {
+    {16, 64, 4, 3.657, 0.6504, 0.0066, 0.7890, 0.0, 0.058, 1.096, 1.507},
+    {16, 32, 4, 3.190, 0.4068, 0.0086, 0.3893, 0.0, 0.109, 1.059, 1.527},
+    {32, 64, 4, 4.100, 0.7969, 0.0032, 0.8843, 0.0038, 0.331, 1.072, 1.332},
+    {128, 256, 1, 4.310, 0.7281, 0.0058, 0.8467, 0.0090, 0.389, 1.123, 1.211},
+    {64, 128, 4, 4.264, 1.1520, 0.0142, 1.6220, 0.0193, 3.724, 1.106, 1.239},
+    {128, 128, 2, 4.047, 0.7302, 0.0096, 0.9289, 0.0119, 2.575, 1.094, 1.244},
+};
+constexpr int kGroupedFormCount = sizeof(kGroupedForms) / sizeof(kGroupedForms[0]);
+
+const GroupedForm& choose_form(int64_t rows, int64_t groups, int64_t N, int64_t K, bool gated, int format)
 {
-    const int64_t each = rows / (groups < rows ? groups : rows);
-    return each <= 12 ? 16 : each <= 24 ? 32 : each <= 48 ? 64 : 128;
+    const int force = knob(Knob::grouped_form);
+    if (force >= 1 && force <= kGroupedFormCount) return kGroupedForms[force - 1];
+    const double used = fmax(1.0, groups * (1.0 - exp(-(double)rows / groups)));
+    const GroupedForm* best = kGroupedForms;
+    double least = 0;
+    for (const GroupedForm& f : kGroupedForms) {
+        const int64_t columns = gated ? f.columns / 2 : f.columns, out = gated ? N / 2 : N;
+        const double tiles = fmax(used, rows / (double)f.height + 0.5 * used), w = tiles * ((out + columns - 1) / columns) / 256;
+        const double r = rows / tiles, k = K / 128.0 / f.parts * (format == kGroupedBf16 ? f.bf16 : format == kGroupedE8 ? f.e8 : 1.0);
+        const double us = f.start + k * fmax(f.one + f.one_row * r, (f.full + f.full_row * r) * w) + f.each * w;
+        if (&f == kGroupedForms || us < least) {
+            least = us;
+            best = &f;
+        }
+    }
+    return *best;
 }
 
 int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K, int group,
@@ -67,9 +106,9 @@ int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows,
     a.group = group;
     a.swiglu = epilogue == E0M4_EPILOGUE_SWIGLU;
     a.Y = Y;
-    const int force = knob(Knob::grouped_tile);
-    const int height = force == 16 || force == 32 || force == 64 || force == 128 ? force : grouped_height(rows, groups);
-    return height == 128 ? launch_grouped_many(a, format, knob(Knob::grouped_exact), (hipStream_t)stream) : launch_grouped_few(a, format, height, (hipStream_t)stream);
+    const GroupedForm& f = choose_form(rows, groups, N, K, a.swiglu, format);
+    return f.height >= 64 ? launch_grouped_many(a, format, f.height, f.columns, (hipStream_t)stream)
+                          : launch_grouped_few(a, format, f.height, f.columns / kBlockRows, (hipStream_t)stream);
 }
 
 int check_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)

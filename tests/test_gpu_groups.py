@@ -133,9 +133,9 @@ CASES = [                                              # format, group, N, K, ro
 ]
 
 
-@pytest.mark.parametrize("tile", [0, 16, 32, 64, 128])
+@pytest.mark.parametrize("form", range(7))
 @pytest.mark.parametrize("fmt,group,N,K,sizes,gated", CASES)
-def test_products(e0m4, fmt, group, N, K, sizes, gated, tile):
+def test_products(e0m4, fmt, group, N, K, sizes, gated, form):
     g, groups = gen(N + K), len(sizes)
     codes, values, scales = make_weights(e0m4, fmt, groups, N, K, group, N)
     index = torch.cat([torch.full((n,), e, dtype=torch.int32) for e, n in enumerate(sizes)] + [torch.full((3,), -1, dtype=torch.int32)])
@@ -148,7 +148,7 @@ def test_products(e0m4, fmt, group, N, K, sizes, gated, tile):
     call = {"e0m4": e0m4.e0m4_matmul_grouped, "e0m8": e0m4.e0m8_matmul_grouped, "bf16": e0m4.e0m4_bf16_matmul_grouped}[fmt]
     epilogue = e0m4.E0M4_EPILOGUE_SWIGLU if gated else e0m4.E0M4_EPILOGUE_NONE
     try:
-        e0m4.e0m4_set_knob("grouped_tile", tile)
+        e0m4.e0m4_set_knob("grouped_form", form)
         for share in (0, 1):
             at = order.long()[:inside] if share else torch.arange(inside)
             want, bound = plain.products(X, at, groups_of, values, scales, group, gated)
@@ -162,11 +162,11 @@ def test_products(e0m4, fmt, group, N, K, sizes, gated, tile):
             again = call(poisoned.to(DEV), plan, codes, N, K, group, share=share, epilogue=epilogue)
             assert torch.equal(again[:inside], out[:inside])
     finally:
-        e0m4.e0m4_set_knob("grouped_tile", 0)
+        e0m4.e0m4_set_knob("grouped_form", 0)
 
 
-@pytest.mark.parametrize("tile", [16, 128])
-def test_products_of_gathered_rows_that_several_entries_share(e0m4, tile):
+@pytest.mark.parametrize("form", [1, 4])
+def test_products_of_gathered_rows_that_several_entries_share(e0m4, form):
     groups, N, K, tokens, k = 6, 128, 256, 45, 3
     g = gen(3)
     codes, values, scales = make_weights(e0m4, "e0m4", groups, N, K, 128, 5)
@@ -175,15 +175,15 @@ def test_products_of_gathered_rows_that_several_entries_share(e0m4, tile):
     _, order, _ = plain.layout(index, groups)
     X = torch.randn((tokens, K), generator=g).half()
     want, bound = plain.products(X, order.long() // k, index.flatten()[order.long()].tolist(), values, scales, 128, False)
-    e0m4.e0m4_set_knob("grouped_tile", tile)
+    e0m4.e0m4_set_knob("grouped_form", form)
     try:
         within(e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 128, share=k), want, bound)
     finally:
-        e0m4.e0m4_set_knob("grouped_tile", 0)
+        e0m4.e0m4_set_knob("grouped_form", 0)
 
 
-@pytest.mark.parametrize("tile", [16, 32, 64, 128])
-def test_nan_and_infinity_stay_in_their_row(e0m4, tile):
+@pytest.mark.parametrize("form", range(1, 7))
+def test_nan_and_infinity_stay_in_their_row(e0m4, form):
     N, K = 64, 160                                      # (the last k block is not whole: what lies behind a row is the next one's)
     codes, values, scales = make_weights(e0m4, "e0m4", 2, N, K, 32, 9)
     index = torch.tensor([0] * 20 + [1] * 13, dtype=torch.int32)
@@ -191,12 +191,12 @@ def test_nan_and_infinity_stay_in_their_row(e0m4, tile):
     X = torch.randn((33, K), generator=gen(2)).half()
     clean = e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 32, share=1)
     X[4, 0], X[25, 3], X[32, K - 1] = float("nan"), float("inf"), float("nan")
-    e0m4.e0m4_set_knob("grouped_tile", tile)
+    e0m4.e0m4_set_knob("grouped_form", form)
     try:
         want = e0m4.e0m4_matmul_grouped(torch.where(torch.isfinite(X), X, 0).to(DEV), plan, codes, N, K, 32, share=1)
         got = e0m4.e0m4_matmul_grouped(X.to(DEV), plan, codes, N, K, 32, share=1)
     finally:
-        e0m4.e0m4_set_knob("grouped_tile", 0)
+        e0m4.e0m4_set_knob("grouped_form", 0)
     touched = torch.zeros(33, dtype=torch.bool)
     touched[[4, 25, 32]] = True
     assert torch.equal(got[~touched.to(DEV)], want[~touched.to(DEV)])
