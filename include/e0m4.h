@@ -520,9 +520,9 @@ int e0m4_route(const void* logits, int dtype, int64_t tokens, int64_t experts, i
  * groups' weights [N, K] one after the other, each of e0m4_codes_bytes(N, K, group)
  * (e0m8_codes_bytes) bytes.  N <= 2^24, 0 < K, K as for e0m4_matmul (e0m8_matmul), with
  * share > 0 X of less than 2 GiB, gated the gate's half of a buffer of at most 1 GiB.
- * Accumulation is fp32; tiles of many rows, and groups of 32 and 64, multiply weights
- * rounded as e0m4_dequant rounds them, the others the codes' exact values.  Y may not
- * overlap X.  No workspace.
+ * Accumulation is fp32; every weight is rounded to 16 bits as the dequant entry points do.  Y may not
+ * overlap X.  No workspace.  A call whose tiles times column blocks would not fit one launch (2^32
+ * work items, more than 3e11 outputs) is refused (E0M4_ERR_SHAPE).
  */
 int e0m4_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
                         int group, int epilogue, void* Y_f16, void* stream);

@@ -558,6 +558,14 @@ def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups
     return E0M4Groups(_empty(need // 4, torch.int32, device, stream, "plan"), rows, groups)
 
 
+def _on_device(where: str, *tensors):
+    """Launches go to the current device, so what they read and write has to be there."""
+    current = _current_device() if _current_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError("%s: a tensor is on %s, but the current device is cuda:%d" % (where, t.device, current))
+
+
 def _groups_plan(plan, rows, groups, where: str):
     """The plan's pointer, checked (rows, groups None: any)."""
     data, r, g = plan
@@ -575,6 +583,7 @@ def e0m4_groups(index: torch.Tensor, groups: int, plan: E0M4Groups = None, strea
     _need(index, torch.int32, index.shape, "index")
     if plan is None:
         plan = e0m4_groups_alloc(rows, groups, index.device, stream)
+    _on_device("e0m4_groups", index, plan.data)
     _check(lib().e0m4_groups(_ptr(index), rows, groups, _groups_plan(plan, rows, groups, "e0m4_groups"), _stream(stream)), "e0m4_groups")
     return plan
 
@@ -596,6 +605,7 @@ def e0m4_route(logits: torch.Tensor, k: int, scoring: int = E0M4_ROUTE_SOFTMAX, 
         pointer = plan.data.data_ptr()
     else:
         pointer = _groups_plan(plan, tokens * k, experts, "e0m4_route")
+    _on_device("e0m4_route", logits, count, plan.data)
     chosen = _empty((tokens, k), torch.int32, device, stream, "chosen")
     weights = _empty((tokens, k), torch.float32, device, stream, "weights")
     _check(lib().e0m4_route(logits.data_ptr(), _DTYPES[logits.dtype], tokens, experts, logits.stride(0), k, scoring, 1 if renormalise else 0, factor,
@@ -617,6 +627,7 @@ def _matmul_grouped(call: str, codes_bytes, dtype, X, plan, codes, N, K, group, 
         out = _empty((rows, n_out), dtype, X.device, stream, "out")
     else:
         _need(out, dtype, (rows, n_out), "out")
+    _on_device(call, X, plan.data, codes, out)
     _check(getattr(lib(), call)(X.data_ptr(), share, pointer, rows, groups, codes.data_ptr(), N, K, group, epilogue, out.data_ptr(), _stream(stream)), call)
     return out
 
@@ -652,8 +663,9 @@ def e0m4_combine(Y, weights, plan: E0M4Groups, base=None, out=None, stream=None)
         out = _empty((tokens, N), Y.dtype, Y.device, stream, "out")
     else:
         _need(out, Y.dtype, (tokens, N), "out")
-    _check(lib().e0m4_combine(Y.data_ptr(), _DTYPES[Y.dtype], N, weights.data_ptr(), _groups_plan(plan, tokens * k, None, "e0m4_combine"), tokens, k,
-                              plan.groups, _ptr(base), out.data_ptr(), _stream(stream)), "e0m4_combine")
+    pointer = _groups_plan(plan, tokens * k, None, "e0m4_combine")
+    _on_device("e0m4_combine", Y, weights, plan.data, base, out)
+    _check(lib().e0m4_combine(Y.data_ptr(), _DTYPES[Y.dtype], N, weights.data_ptr(), pointer, tokens, k, plan.groups, _ptr(base), out.data_ptr(), _stream(stream)), "e0m4_combine")
     return out
 
 
@@ -691,7 +703,9 @@ def e0m4_lora(X, plan: E0M4Groups, A, B, factors=None, base=None, out=None, work
         if need > 0:
             workspace = _empty(need, torch.uint8, X.device, stream, "workspace")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().e0m4_lora(X.data_ptr(), x_ld, _DTYPES[dtype], _groups_plan(plan, rows, adapters, "e0m4_lora"), rows, adapters, A.data_ptr(), B.data_ptr(), rank,
+    pointer = _groups_plan(plan, rows, adapters, "e0m4_lora")
+    _on_device("e0m4_lora", X, plan.data, A, B, factors, base, out, workspace)
+    _check(lib().e0m4_lora(X.data_ptr(), x_ld, _DTYPES[dtype], pointer, rows, adapters, A.data_ptr(), B.data_ptr(), rank,
                            _ptr(factors), N, K, _ptr(base), base_ld, out.data_ptr(), out_ld, _ptr(workspace), ws_bytes, _stream(stream)), "e0m4_lora")
     return out
 

@@ -20,6 +20,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kWavesL = 4, kThreadsL = kWavesL * 64;
 constexpr int kChunkK = 128;                    // k of a wavefront's turn
+constexpr int64_t kCopyWorkgroups = 256;        // for rows without an adapter
 constexpr uint32_t kNowhere = 0x80000000u;      // beyond a buffer's end, whatever is added to it
 
 template <bool BF>
@@ -382,7 +383,6 @@ template <bool BF, int MT, int NT>
 int launch_shrink(const LoraArgs& a, const LoraPlan& p, float* H, hipStream_t stream)
 {
     const int64_t grid = p.shrink_tiles * p.splits;
-    if (grid * kThreadsL > 0xffffffffLL) return E0M4_ERR_SHAPE;
     constexpr int lds = kWavesL * (MT + NT) * 16 * kChunkRowBytes;
     static_assert(lds >= (kWavesL - 1) * NT * MT * 1024 && lds <= 160 * 1024, "sums fit, and all fits the LDS of a compute unit");
     static std::atomic<uint64_t> lds_allowed{0};
@@ -397,8 +397,7 @@ int launch_expand(const LoraArgs& a, const LoraPlan& p, const float* H, hipStrea
 {
     const int64_t tiles = p.expand_tiles * p.columns;
     // (in place, with the same rows: nothing to copy)
-    const int64_t grid = tiles + (a.base == a.out ? 0 : std::min<int64_t>(a.rows, 256));
-    if (grid * kThreadsL > 0xffffffffLL) return E0M4_ERR_SHAPE;
+    const int64_t grid = tiles + (a.base == a.out ? 0 : std::min<int64_t>(a.rows, kCopyWorkgroups));
     constexpr int lds = expand_lds(MT, NT);
     static_assert(lds <= 160 * 1024, "the LDS of a compute unit");
     static std::atomic<uint64_t> lds_allowed{0};
@@ -436,6 +435,8 @@ size_t lora_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N,
 int launch_lora(const LoraArgs& a, void* workspace, hipStream_t stream)
 {
     const LoraPlan p = plan_lora(a.rows, a.adapters, a.rank, a.N, a.K);
+    // (both launches fit their grids, or neither goes out)
+    if (p.shrink_tiles * p.splits * kThreadsL > 0xffffffffLL || (p.expand_tiles * p.columns + kCopyWorkgroups) * kThreadsL > 0xffffffffLL) return E0M4_ERR_SHAPE;
     float* H = static_cast<float*>(workspace);
     const int rc = with_sizes(a.dtype == E0M4_BF16, p.shrink_height, a.rank, [&](auto bf, auto mt, auto nt) -> int {
         if constexpr (decltype(mt)::value > 1 && decltype(nt)::value == 8) return E0M4_ERR_SHAPE;

@@ -7,6 +7,8 @@ projection adds the residual.  The attention collects what every cached row rece
 least leave it (e0m4_kv4_evict) and the tokens go on from there.  There is no rotary embedding here: a model that has one turns
 queries and keys between the projection and the append, by the number of tokens that came before and not by the rows in the cache,
 which are fewer after an eviction; rows in the cache keep the angle of their own token.
+
+Sequences of different users can have low-rank adapters of their own beside the output projection that they share (add_adapters, e0m4_lora).
 """
 from __future__ import annotations
 
@@ -16,6 +18,8 @@ from . import binding as e0m4
 
 
 class Kv4AttentionBlock:
+    adapters = None                                     # (A, B, factors) of the output projection's, or None
+
     def __init__(self, heads: int, kv_heads: int, dim: int, batch: int, capacity: int, budget: int, recent: int, group: int = 128, cache_group: int = 64,
                  seed: int = 0, device="cuda"):
         """Rows leave a full cache of `capacity` down to `budget`, the newest `recent` never."""
@@ -35,6 +39,12 @@ class Kv4AttentionBlock:
         self.lengths = torch.zeros(batch, dtype=torch.int32, device=device)
         self.most = 0                                   # rows of the longest sequence, known without asking the device
 
+    def add_adapters(self, A: torch.Tensor, B: torch.Tensor, factors: torch.Tensor = None):
+        """Low-rank adapters of the output projection: A [adapters, rank, hidden], B [adapters, hidden, rank] fp16, factors fp32 [adapters]."""
+        if A.dim() != 3 or B.shape != (A.shape[0], self.hidden, A.shape[1]) or A.shape[2] != self.hidden:
+            raise ValueError("A must be [adapters, rank, %d] and B [adapters, %d, rank], got %s and %s" % (self.hidden, self.hidden, tuple(A.shape), tuple(B.shape)))
+        self.adapters = (A, B, factors)
+
     def evict(self):
         kept, self.lengths, received = e0m4.e0m4_kv4_evict(self.cache, self.shape, self.received, self.lengths, self.budget, self.recent,
                                                            self.other, self.shape)
@@ -44,14 +54,17 @@ class Kv4AttentionBlock:
         self.most = min(self.most, self.budget)
         return kept
 
-    def __call__(self, x: torch.Tensor) -> torch.Tensor:
-        """x [batch, n, hidden] fp16, the next n tokens of every sequence -> the block's output, of the same shape."""
+    def __call__(self, x: torch.Tensor, adapter: torch.Tensor = None) -> torch.Tensor:
+        """x [batch, n, hidden] fp16, the next n tokens of every sequence -> the block's output, of the same shape.  adapter: int32 [batch] on
+        the device, each sequence's adapter (-1: none)."""
         batch, n, hidden = x.shape
         if batch != self.shape.batch or hidden != self.hidden:
             raise ValueError("x must be [%d, n, %d], got %s" % (self.shape.batch, self.hidden, tuple(x.shape)))
         # (all that can refuse the call comes before the eviction: rows that left are gone)
         if min(self.most, self.budget) + n > self.shape.capacity:
             raise ValueError("%d tokens do not fit behind the %d rows that stay" % (n, min(self.most, self.budget)))
+        if adapter is not None and (self.adapters is None or adapter.shape != (batch,) or adapter.dtype != torch.int32):
+            raise ValueError("adapter must be int32 [%d], for a block that has adapters" % batch)
         flat = x.reshape(batch * n, hidden)
         qkv = e0m4.e0m4_matmul_fused(flat, self.qkv, self.columns, hidden, self.group, rms_gamma=self.gamma, rms_eps=1e-5)
         if self.most + n > self.shape.capacity:
@@ -62,7 +75,13 @@ class Kv4AttentionBlock:
         self.lengths = self.lengths + n
         self.most += n
         attended = e0m4.e0m4_kv4_attention(q, self.cache, self.shape, self.lengths, weights=self.received)
-        return e0m4.e0m4_matmul_fused(attended.view(batch * n, hidden), self.out, hidden, hidden, self.group, residual=flat).view(x.shape)
+        attended = attended.view(batch * n, hidden)
+        y = e0m4.e0m4_matmul_fused(attended, self.out, hidden, hidden, self.group, residual=flat)
+        if adapter is not None and n > 0:
+            A, B, factors = self.adapters
+            plan = e0m4.e0m4_groups(adapter.repeat_interleave(n), A.shape[0])
+            e0m4.e0m4_lora(attended, plan, A, B, factors=factors, base=y, out=y)
+        return y.view(x.shape)
 
 
 def main():
