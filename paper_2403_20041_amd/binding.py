@@ -558,33 +558,44 @@ def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups
     return E0M4Groups(_empty(need // 4, torch.int32, device, stream, "plan"), rows, groups)
 
 
-def _on_device(where: str, *tensors):
-    """Launches go to the current device, so what they read and write has to be there."""
-    current = _current_device() if _current_device is not None else torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != current:
-            raise ValueError("%s: a tensor is on %s, but the current device is cuda:%d" % (where, t.device, current))
+def _here(where: str, first: torch.Tensor) -> int:
+    """The current device, for the checks of a call: launches go to it, so what they read and write has to be there."""
+    if not first.is_cuda:
+        raise ValueError("%s: tensors must be on the GPU, got one on %s" % (where, first.device))
+    return _current_device() if _current_device is not None else torch.cuda.current_device()
 
 
-def _groups_plan(plan, rows, groups, where: str):
+def _need_here(t: torch.Tensor, dtype, shape, name: str, here: int):
+    """_need, and on the current device."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != here or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on the current device, cuda:%d, got %s %s on %s"
+                         % (name, dtype, tuple(shape), here, t.dtype, tuple(t.shape), t.device))
+
+
+def _new(like: torch.Tensor, shape, stream, what: str):
+    """_empty of the type and device of `like`."""
+    return like.new_empty(shape) if stream is None else _empty(shape, like.dtype, like.device, stream, what)
+
+
+def _groups_plan(plan, rows, groups, where: str, here: int):
     """The plan's pointer, checked (rows, groups None: any)."""
     data, r, g = plan
     need = _groups_bytes(r, g)
-    if need == 0 or data.dtype is not torch.int32 or not data.is_contiguous() or not data.is_cuda or data.numel() * 4 < need or \
+    if need == 0 or data.dtype is not torch.int32 or not data.is_contiguous() or data.get_device() != here or data.numel() * 4 < need or \
             (rows is not None and r != rows) or (groups is not None and g != groups):
-        raise ValueError("%s: plan must be a layout of %s rows and %s groups on the GPU, got one of %d and %d with %d elements of %s"
-                         % (where, "any" if rows is None else rows, "any" if groups is None else groups, r, g, data.numel(), data.dtype))
+        raise ValueError("%s: plan must be a layout of %s rows and %s groups on the current device, got one of %d and %d with %d elements of %s on %s"
+                         % (where, "any" if rows is None else rows, "any" if groups is None else groups, r, g, data.numel(), data.dtype, data.device))
     return data.data_ptr()
 
 
 def e0m4_groups(index: torch.Tensor, groups: int, plan: E0M4Groups = None, stream=None) -> E0M4Groups:
     """The layout of entries by index (int32, any shape; values outside [0, groups) choose none)."""
-    rows = index.numel()
-    _need(index, torch.int32, index.shape, "index")
+    where = "e0m4_groups"
+    rows, here = index.numel(), _here(where, index)
+    _need_here(index, torch.int32, index.shape, "index", here)
     if plan is None:
         plan = e0m4_groups_alloc(rows, groups, index.device, stream)
-    _on_device("e0m4_groups", index, plan.data)
-    _check(lib().e0m4_groups(_ptr(index), rows, groups, _groups_plan(plan, rows, groups, "e0m4_groups"), _stream(stream)), "e0m4_groups")
+    _check(lib().e0m4_groups(index.data_ptr(), rows, groups, _groups_plan(plan, rows, groups, where, here), _stream(stream)), where)
     return plan
 
 
@@ -592,42 +603,42 @@ def e0m4_route(logits: torch.Tensor, k: int, scoring: int = E0M4_ROUTE_SOFTMAX, 
                plan: E0M4Groups = None, stream=None):
     """logits [tokens, experts] (fp16, bf16 or fp32, rows at any distance) -> (chosen int32 [tokens, k], weights fp32 [tokens, k], the
     entries' layout by expert).  count: int32 [1] on the device, tokens from there on choose none."""
+    where = "e0m4_route"
     tokens, experts = logits.shape
     if logits.dtype not in _DTYPES:
         raise TypeError("e0m4_route: logits must be float16, bfloat16 or float32")
-    if not logits.is_cuda or (logits.numel() and experts > 1 and logits.stride(1) != 1):
-        raise ValueError("e0m4_route: logits must be a cuda tensor whose rows are contiguous")
+    here = _here(where, logits)
+    distance, apart = logits.stride()
+    if logits.get_device() != here or (apart != 1 and logits.numel() and experts > 1):
+        raise ValueError("e0m4_route: logits must be a tensor on the current device whose rows are contiguous")
     if count is not None:
-        _need(count, torch.int32, (1,), "count")
+        _need_here(count, torch.int32, (1,), "count", here)
     device = logits.device
     if plan is None:
         plan = e0m4_groups_alloc(tokens * k, experts, device, stream)
-        pointer = plan.data.data_ptr()
-    else:
-        pointer = _groups_plan(plan, tokens * k, experts, "e0m4_route")
-    _on_device("e0m4_route", logits, count, plan.data)
+    pointer = _groups_plan(plan, tokens * k, experts, where, here)
     chosen = _empty((tokens, k), torch.int32, device, stream, "chosen")
     weights = _empty((tokens, k), torch.float32, device, stream, "weights")
-    _check(lib().e0m4_route(logits.data_ptr(), _DTYPES[logits.dtype], tokens, experts, logits.stride(0), k, scoring, 1 if renormalise else 0, factor,
-                            _ptr(count), chosen.data_ptr(), weights.data_ptr(), pointer, _stream(stream)), "e0m4_route")
+    _check(lib().e0m4_route(logits.data_ptr(), _DTYPES[logits.dtype], tokens, experts, distance, k, scoring, 1 if renormalise else 0, factor,
+                            _ptr(count), chosen.data_ptr(), weights.data_ptr(), pointer, _stream(stream)), where)
     return chosen, weights, plan
 
 
 def _matmul_grouped(call: str, codes_bytes, dtype, X, plan, codes, N, K, group, share, epilogue, out, stream):
     rows, groups = plan.rows, plan.groups
-    pointer = _groups_plan(plan, None, None, call)
+    here = _here(call, X)
+    pointer = _groups_plan(plan, None, None, call, here)
     if share < 0 or (share > 0 and rows % share):
         raise ValueError("%s: %d entries are not a whole number for each row with share = %d" % (call, rows, share))
-    _need(X, dtype, (rows // share if share else rows, K), "X")
+    _need_here(X, dtype, (rows // share if share else rows, K), "X", here)
     need = groups * codes_bytes(N, K, group)
-    if codes.dtype is not torch.uint8 or not codes.is_contiguous() or not codes.is_cuda or codes.numel() < need:
-        raise ValueError("%s: codes must be a contiguous cuda uint8 tensor of at least %d bytes" % (call, need))
+    if codes.dtype is not torch.uint8 or not codes.is_contiguous() or codes.get_device() != here or codes.numel() < need:
+        raise ValueError("%s: codes must be a contiguous uint8 tensor of at least %d bytes on the current device" % (call, need))
     n_out = N // 2 if epilogue == E0M4_EPILOGUE_SWIGLU else N
     if out is None:
-        out = _empty((rows, n_out), dtype, X.device, stream, "out")
+        out = _new(X, (rows, n_out), stream, "out")
     else:
-        _need(out, dtype, (rows, n_out), "out")
-    _on_device(call, X, plan.data, codes, out)
+        _need_here(out, dtype, (rows, n_out), "out", here)
     _check(getattr(lib(), call)(X.data_ptr(), share, pointer, rows, groups, codes.data_ptr(), N, K, group, epilogue, out.data_ptr(), _stream(stream)), call)
     return out
 
@@ -651,30 +662,32 @@ def e0m4_bf16_matmul_grouped(X, plan: E0M4Groups, codes, N: int, K: int, group: 
 
 def e0m4_combine(Y, weights, plan: E0M4Groups, base=None, out=None, stream=None) -> torch.Tensor:
     """out [tokens, N] = base + the sum of each token's rows of Y [tokens * k, N] (in the layout's order) times weights fp32 [tokens, k]."""
-    tokens, k = weights.shape
-    N = Y.shape[1]
-    if Y.dtype not in _KV4_DTYPES:
+    where = "e0m4_combine"
+    tokens, k = size = weights.shape
+    N, dtype = Y.shape[1], Y.dtype
+    if dtype not in _KV4_DTYPES:
         raise TypeError("e0m4_combine: Y must be float16 or bfloat16")
-    _need(weights, torch.float32, (tokens, k), "weights")
-    _need(Y, Y.dtype, (tokens * k, N), "Y")
+    here = _here(where, Y)
+    _need_here(weights, torch.float32, size, "weights", here)
+    _need_here(Y, dtype, (tokens * k, N), "Y", here)
     if base is not None:
-        _need(base, Y.dtype, (tokens, N), "base")
+        _need_here(base, dtype, (tokens, N), "base", here)
     if out is None:
-        out = _empty((tokens, N), Y.dtype, Y.device, stream, "out")
+        out = _new(Y, (tokens, N), stream, "out")
     else:
-        _need(out, Y.dtype, (tokens, N), "out")
-    pointer = _groups_plan(plan, tokens * k, None, "e0m4_combine")
-    _on_device("e0m4_combine", Y, weights, plan.data, base, out)
-    _check(lib().e0m4_combine(Y.data_ptr(), _DTYPES[Y.dtype], N, weights.data_ptr(), pointer, tokens, k, plan.groups, _ptr(base), out.data_ptr(), _stream(stream)), "e0m4_combine")
+        _need_here(out, dtype, (tokens, N), "out", here)
+    _check(lib().e0m4_combine(Y.data_ptr(), _DTYPES[dtype], N, weights.data_ptr(), _groups_plan(plan, tokens * k, None, where, here), tokens, k, plan.groups,
+                              _ptr(base), out.data_ptr(), _stream(stream)), where)
     return out
 
 
-def _lora_rows(t, dtype, shape, name: str) -> int:
+def _lora_rows(t, dtype, shape, name: str, here: int) -> int:
     """The distance of the rows of a [rows, columns] tensor whose columns are contiguous."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.numel() and shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("e0m4_lora: %s must be a cuda %s tensor of shape %s with contiguous rows, got %s %s with strides %s on %s"
+    distance, apart = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != here or (apart != 1 and shape[1] > 1 and t.numel()):
+        raise ValueError("e0m4_lora: %s must be a %s tensor of shape %s with contiguous rows on the current device, got %s %s with strides %s on %s"
                          % (name, dtype, tuple(shape), t.dtype, tuple(t.shape), t.stride(), t.device))
-    return t.stride(0) if shape[0] > 1 else shape[1]
+    return distance if shape[0] > 1 else shape[1]
 
 
 @functools.lru_cache(maxsize=1024)
@@ -685,28 +698,34 @@ def e0m4_lora_workspace_bytes(rows: int, adapters: int, rank: int, N: int, K: in
 def e0m4_lora(X, plan: E0M4Groups, A, B, factors=None, base=None, out=None, workspace=None, stream=None) -> torch.Tensor:
     """out [rows, N] = base + factors[a] * B[a] (A[a] x) for each row's adapter a, the layout's group of the row; rows of no group keep their base.  X [rows, K],
     A [adapters, rank, K], B [adapters, N, rank], all fp16 or bf16; X, base and out may be columns of wider matrices; out may be base."""
-    adapters, rank, K = A.shape
+    where = "e0m4_lora"
+    adapters, rank, K = a_size = A.shape
     rows, N, dtype = X.shape[0], B.shape[1], X.dtype
     if dtype not in _KV4_DTYPES:
         raise TypeError("e0m4_lora: X must be float16 or bfloat16")
-    x_ld = _lora_rows(X, dtype, (rows, K), "X")
-    _need(A, dtype, (adapters, rank, K), "A")
-    _need(B, dtype, (adapters, N, rank), "B")
+    here = _here(where, X)
+    x_ld = _lora_rows(X, dtype, (rows, K), "X", here)
+    _need_here(A, dtype, a_size, "A", here)
+    _need_here(B, dtype, (adapters, N, rank), "B", here)
     if factors is not None:
-        _need(factors, torch.float32, (adapters,), "factors")
-    base_ld = _lora_rows(base, dtype, (rows, N), "base") if base is not None else 0
+        _need_here(factors, torch.float32, (adapters,), "factors", here)
+    size = (rows, N)
+    base_ld = _lora_rows(base, dtype, size, "base", here) if base is not None else 0
     if out is None:
-        out = _empty((rows, N), dtype, X.device, stream, "out")
-    out_ld = _lora_rows(out, dtype, (rows, N), "out")
+        out, out_ld = _new(X, size, stream, "out"), N
+    else:
+        out_ld = _lora_rows(out, dtype, size, "out", here)
     if workspace is None:
         need = e0m4_lora_workspace_bytes(rows, adapters, rank, N, K)
+        ws_bytes = need
         if need > 0:
-            workspace = _empty(need, torch.uint8, X.device, stream, "workspace")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    pointer = _groups_plan(plan, rows, adapters, "e0m4_lora")
-    _on_device("e0m4_lora", X, plan.data, A, B, factors, base, out, workspace)
-    _check(lib().e0m4_lora(X.data_ptr(), x_ld, _DTYPES[dtype], pointer, rows, adapters, A.data_ptr(), B.data_ptr(), rank,
-                           _ptr(factors), N, K, _ptr(base), base_ld, out.data_ptr(), out_ld, _ptr(workspace), ws_bytes, _stream(stream)), "e0m4_lora")
+            workspace = _new(A, (need // 2,), stream, "workspace")      # (of a 16-bit type)
+    else:
+        if workspace.get_device() != here:
+            raise ValueError("e0m4_lora: workspace must be on the current device")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _check(lib().e0m4_lora(X.data_ptr(), x_ld, _DTYPES[dtype], _groups_plan(plan, rows, adapters, where, here), rows, adapters, A.data_ptr(), B.data_ptr(), rank,
+                           _ptr(factors), N, K, _ptr(base), base_ld, out.data_ptr(), out_ld, _ptr(workspace), ws_bytes, _stream(stream)), where)
     return out
 
 
