@@ -334,3 +334,55 @@ def test_two_streams_at_once(e0m4):
     for i in range(2):
         for y in got[i]:
             assert torch.equal(y, want[i])
+
+
+@pytest.mark.parametrize("rows", [1, 40, 2000])
+def test_no_row_chooses(e0m4, rows):
+    """All entries of no group: products leave their output as it was, sums and adapters pass the base on."""
+    index = torch.full((rows,), -1, dtype=torch.int32, device=DEV)
+    plan = e0m4.e0m4_groups(index, 4)
+    codes = make_weights(e0m4, "e0m4", 4, 64, 128, 128, 3)[0]
+    X = torch.full((rows, 128), float("nan"), dtype=torch.float16, device=DEV)
+    for form in range(1, 7):
+        e0m4.e0m4_set_knob("grouped_form", form)
+        out = torch.full((rows, 64), 5.0, dtype=torch.float16, device=DEV)
+        e0m4.e0m4_matmul_grouped(X, plan, codes, 64, 128, 128, share=1, out=out)
+        e0m4.e0m4_set_knob("grouped_form", 0)
+        assert (out == 5.0).all()
+    base = torch.randn((rows, 64), generator=gen(1)).half().to(DEV)
+    assert torch.equal(e0m4.e0m4_combine(X[:, :64].contiguous(), torch.ones((rows, 1), device=DEV), plan, base=base), base)
+    A, B = torch.zeros((4, 8, 128), dtype=torch.float16, device=DEV), torch.zeros((4, 64, 8), dtype=torch.float16, device=DEV)
+    assert torch.equal(e0m4.e0m4_lora(X, plan, A, B, base=base), base)
+
+
+def test_empty_problems(e0m4):
+    none = torch.zeros((0, 4), device=DEV)
+    chosen, weights, plan = e0m4.e0m4_route(none, 2)
+    assert chosen.shape == weights.shape == (0, 2) and plan.offsets.tolist() == [0] * 5
+    codes = make_weights(e0m4, "e0m4", 4, 64, 128, 128, 3)[0]
+    x = torch.zeros((0, 128), dtype=torch.float16, device=DEV)
+    y = e0m4.e0m4_matmul_grouped(x, plan, codes, 64, 128, 128, share=2)
+    assert y.shape == (0, 64) and e0m4.e0m4_combine(y, weights, plan).shape == (0, 64)
+    assert e0m4.e0m4_lora(x, e0m4.e0m4_groups(torch.zeros(0, dtype=torch.int32, device=DEV), 3), torch.zeros((3, 8, 128), dtype=torch.float16, device=DEV),
+                          torch.zeros((3, 64, 8), dtype=torch.float16, device=DEV)).shape == (0, 64)
+
+
+def test_caller_owned_buffers_on_another_stream(e0m4):
+    """Everything enqueued on a stream that is not the current one, as a handle, into buffers of the caller's."""
+    experts, k, N, K, tokens = 8, 2, 128, 256, 50
+    codes, values, scales = make_weights(e0m4, "e0m4", experts, N, K, 128, 1)
+    x, logits = torch.randn((tokens, K), generator=gen(1)).half().to(DEV), torch.randn((tokens, experts), generator=gen(2)).to(DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    chosen, weights, plan = e0m4.e0m4_route(logits, k, stream=side)
+    y = e0m4.e0m4_matmul_grouped(x, plan, codes, N, K, 128, share=k, stream=side)
+    out = e0m4.e0m4_combine(y, weights, plan, stream=side)
+    with pytest.raises(ValueError):                     # (a raw handle: the library's buffers would belong to another stream)
+        e0m4.e0m4_combine(y, weights, plan, stream=side.cuda_stream)
+    again = torch.zeros_like(out)
+    side.synchronize()
+    torch.cuda.synchronize()
+    e0m4.e0m4_combine(y, weights, plan, out=again, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    want = e0m4.e0m4_combine(e0m4.e0m4_matmul_grouped(x, e0m4.e0m4_groups(chosen, experts), codes, N, K, 128, share=k), weights, plan)
+    assert torch.equal(out, want) and torch.equal(again, want)
