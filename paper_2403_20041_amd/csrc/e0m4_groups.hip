@@ -8,8 +8,8 @@
 //
 // Layout: a stable counting sort.  The entries of a group keep their order, so results depend on nothing but the choice: counts are
 // integers, an entry's rank among its like within a wavefront comes from ballots over the bits of its group, and wavefronts and workgroups
-// count in order.  Up to 1024 entries are one workgroup's work (choice, counts, places and tiles in one launch); otherwise a first launch
-// chooses and counts per workgroup, and every workgroup of a second one adds up the counts before its own.
+// count in order.  Up to 1024 entries are one workgroup's work (choice, counts, places and tiles in one launch), of 64 tokens at most, as many as it
+// chooses for at once; otherwise a first launch chooses and counts per workgroup, and every workgroup of a second one adds up the counts before its own.
 // What bounds it: launches, and the chains of a few hundred dependent instructions in each.
 #include "e0m4_groups.h"
 
@@ -21,7 +21,8 @@ namespace {
 
 constexpr int kWg = 1024;                       // threads of a workgroup that lays entries out
 constexpr int kSmallWg = 256;                   // ... of few tokens by few experts: its barriers are cheaper
-constexpr int kSmallTokens = 32;
+constexpr int kSmallTokens = 16;
+constexpr int kOneWorkgroupTokens = 64;         // more tokens to choose for, or entries than threads: two launches
 constexpr int kCountThreads = 512;
 constexpr int kCountEntries = 256;              // entries of a workgroup of the first of two launches, at least
 
@@ -448,7 +449,7 @@ int launch_route_as(const RouteArgs& a, void* plan, hipStream_t stream)
         hipLaunchKernelGGL((route_small_kernel<kSmallWg, LANES, PER, CHOOSE>), dim3(1), dim3(kSmallWg), 0, stream, ROUTE_ARGUMENTS);
         return check_launch();
     }
-    if (plan && rows <= kWg) {
+    if (plan && rows <= kWg && (!CHOOSE || a.tokens <= kOneWorkgroupTokens)) {
         hipLaunchKernelGGL((route_small_kernel<kWg, LANES, PER, CHOOSE>), dim3(1), dim3(kWg), 0, stream, ROUTE_ARGUMENTS);
         return check_launch();
     }

@@ -45,24 +45,26 @@ int check_grouped(int64_t rows, int64_t groups, int64_t share, int64_t N, int64_
 // The forms of the product, and what an estimate of their launches' time goes by, in us: with w the workgroups for each of the 256 compute units, r rows of a
 // tile that exist on average and b k blocks of 128 that a part of a workgroup walks,
 //     start + b * max(one + one_row r, (full + full_row r) w) + each w,
-// b's factor times a format's own.  Workgroups are counted as if every row chose a group at random.
-// The constants are a least-squares fit (logarithm of the ratio to the measurement, rms 11 - 14 %) to 6277 problems, each timed in all forms: 4 to 128
+// one and full each times a factor of bfloat16's or the 8-bit format's own.  Workgroups are counted as if every row chose a group at random.
+// The constants are a least-squares fit (logarithm of the ratio to the measurement, rms 10 - 14 %) to 8803 problems, each timed in all forms: 4 to 128
 // groups, 1 to 250 rows to a group, gated and plain, 512 to 27392 columns, 512 to 14080 weights a row, all formats and groups.  Choosing by the
-// estimate costs 1.9 % over the best form of each (geometric mean); without one of the forms 2.2 - 2.5 %, without the second 6.0, without the
-// fourth 9.0.
+// estimate costs 1.8 % over the best form of each (geometric mean); without one of the forms 2.1 - 2.5 %, without the second 5.5, without the
+// fourth 8.6.  A seventh, 128 x 256 with two parts of K (10 - 15 % less time where the fourth has a workgroup for every second compute unit), would gain 0.2 %
+// on all.
 struct GroupedForm {
     int height;                                         // rows of a tile
     int columns;                                        // weight rows of a workgroup
     int parts;                                          // of K, side by side
-    double start, one, one_row, full, full_row, each, bf16, e8;
+    double start, one, one_row, full, full_row, each;
+    double one_bf16, one_e8, full_bf16, full_e8;
 };
 constexpr GroupedForm kGroupedForms[] = {
-    {16, 64, 4, 3.657, 0.6504, 0.0066, 0.7890, 0.0, 0.058, 1.096, 1.507},
-    {16, 32, 4, 3.190, 0.4068, 0.0086, 0.3893, 0.0, 0.109, 1.059, 1.527},
-    {32, 64, 4, 4.100, 0.7969, 0.0032, 0.8843, 0.0038, 0.331, 1.072, 1.332},
-    {128, 256, 1, 4.310, 0.7281, 0.0058, 0.8467, 0.0090, 0.389, 1.123, 1.211},
-    {64, 128, 4, 4.264, 1.1520, 0.0142, 1.6220, 0.0193, 3.724, 1.106, 1.239},
-    {128, 128, 2, 4.047, 0.7302, 0.0096, 0.9289, 0.0119, 2.575, 1.094, 1.244},
+    {16, 64, 4, 3.653, 0.6849, 0.0060, 0.7829, 0.0, 0.066, 1.138, 1.121, 1.095, 1.562},
+    {16, 32, 4, 3.242, 0.3820, 0.0123, 0.3880, 0.0, 0.112, 1.172, 1.409, 1.056, 1.514},
+    {32, 64, 4, 4.058, 0.8297, 0.0028, 0.8736, 0.0040, 0.354, 1.102, 1.082, 1.066, 1.386},
+    {128, 256, 1, 4.313, 0.7466, 0.0054, 0.8479, 0.0084, 0.327, 1.168, 1.122, 1.091, 1.386},
+    {64, 128, 4, 4.279, 1.1730, 0.0124, 1.5709, 0.0167, 3.818, 1.167, 1.120, 1.123, 1.334},
+    {128, 128, 2, 3.982, 0.7367, 0.0077, 0.9139, 0.0105, 2.610, 1.149, 1.131, 1.101, 1.319},
 };
 constexpr int kGroupedFormCount = sizeof(kGroupedForms) / sizeof(kGroupedForms[0]);
 
@@ -76,8 +78,10 @@ const GroupedForm& choose_form(int64_t rows, int64_t groups, int64_t N, int64_t 
     for (const GroupedForm& f : kGroupedForms) {
         const int64_t columns = gated ? f.columns / 2 : f.columns, out = gated ? N / 2 : N;
         const double tiles = fmax(used, rows / (double)f.height + 0.5 * used), w = tiles * ((out + columns - 1) / columns) / 256;
-        const double r = rows / tiles, k = K / 128.0 / f.parts * (format == kGroupedBf16 ? f.bf16 : format == kGroupedE8 ? f.e8 : 1.0);
-        const double us = f.start + k * fmax(f.one + f.one_row * r, (f.full + f.full_row * r) * w) + f.each * w;
+        const double one = format == kGroupedBf16 ? f.one_bf16 : format == kGroupedE8 ? f.one_e8 : 1.0;
+        const double full = format == kGroupedBf16 ? f.full_bf16 : format == kGroupedE8 ? f.full_e8 : 1.0;
+        const double r = rows / tiles, b = K / 128.0 / f.parts;
+        const double us = f.start + b * fmax((f.one + f.one_row * r) * one, (f.full + f.full_row * r) * w * full) + f.each * w;
         if (&f == kGroupedForms || us < least) {
             least = us;
             best = &f;
