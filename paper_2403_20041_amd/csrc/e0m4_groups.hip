@@ -10,7 +10,8 @@
 // integers, an entry's rank among its like within a wavefront comes from ballots over the bits of its group, and wavefronts and workgroups
 // count in order.  Up to 1024 entries are one workgroup's work (choice, counts, places and tiles in one launch), of 64 tokens at most, as many as it
 // chooses for at once; otherwise a first launch chooses and counts per workgroup, and every workgroup of a second one adds up the counts before its own.
-// What bounds it: launches, and the chains of a few hundred dependent instructions in each.
+// What bounds it: launches, and the chains of a few hundred dependent instructions in each.  One token of 64 experts 4.6 us, 32 of 128 with 8 chosen 8.9, 128
+// 11.1, 4096 13.8 (6.2 the choice, 7.7 the places).
 #include "e0m4_groups.h"
 
 #include <float.h>
@@ -484,7 +485,7 @@ namespace {
 
 constexpr int kCombineThreads = 256;
 
-// A wavefront: 64 pieces of V columns of one token.  All of a token's rows are requested before the first is used; sums in fp32, in the order
+// Bound by memory: 4096 tokens with 8 rows of 2048, bfloat16, 168 MB in 30 us.  A wavefront: 64 pieces of V columns of one token.  All of a token's rows are requested before the first is used; sums in fp32, in the order
 // of the token's choices, one rounding.
 template <typename T, int V>
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const T* __restrict__ Y, const float* __restrict__ weights, const int* __restrict__ place,
