@@ -196,7 +196,8 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
 // MFMAs is column 16 (n/4) + 4 j + n%4, so that a lane's results, 4 q .. + 3 of each, are the columns 16 q .. + 15 of row n.  The 64 rows of B are one piece
 // of memory that comes to LDS as it is, but for the order of 16-byte pieces in a row (see order_of), one set of columns ahead.  With more than 16 rows the wavefronts make the
 // operands of 16 rows each and share them through LDS.
-__host__ __device__ constexpr int expand_lds(int MT, int NT) { return (MT > 1 ? NT * MT * 1024 + MT * 64 : 0) + kWavesL * 2 * 64 * NT * 32; }
+__host__ __device__ constexpr int expand_sets(int NT) { return NT >= 4 ? 1 : 2; }
+__host__ __device__ constexpr int expand_lds(int MT, int NT) { return (MT > 1 ? NT * MT * 1024 + MT * 64 : 0) + kWavesL * expand_sets(NT) * 64 * NT * 32; }
 template <bool BF, int MT, int NT>
 __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* plan, int rows, int adapters, uint32_t columns, uint32_t tile_grid, const float* H, int rank,
                                                                     int splits, const char* B, const float* factors, int N, const char* base, char* out,
@@ -254,7 +255,8 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
         piece_at[e] = r * ppr + (uint32_t)order_of((int)p, (int)r >> 4, (int)r & 3);
     }
     const __amdgpu_buffer_rsrc_t b_rsrc = make_rsrc(B + (int64_t)tile.group * N * rank * 2);
-    unsigned char* w_lds = smem + (kShared ? NT * MT * 1024 + MT * 64 : 0) + wave * (2 * 64 * NT * 32);
+    constexpr int kSets = expand_sets(NT);
+    unsigned char* w_lds = smem + (kShared ? NT * MT * 1024 + MT * 64 : 0) + wave * (kSets * 64 * NT * 32);
     uint32_t w_at[NT];                                  // of step j, MFMA 0 (a row of MFMA j4: 4 j4 rows on); the rank's end: any piece, its operand is zeroed
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
     for (; c0 < N; c0 += step) {
         wait_loads<0>();                                // these columns' rows of B
         __builtin_amdgcn_sched_barrier(0);
-        if (c0 + step < N) load_w(c0 + step, set ^ 1);
+        if (kSets == 2 && c0 + step < N) load_w(c0 + step, set ^ 1);
         __builtin_amdgcn_sched_barrier(0);
         const int col = c0 + 16 * q;                    // this lane's results: columns col .. col + 15 of its rows
         floatx4 acc[4][MT];
@@ -332,6 +334,12 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
                 for (int j4 = 0; j4 < 4; ++j4) acc[j4][i] = mfma16<BF>(w[j4], h, acc[j4][i]);
             }
         }
+        if (kSets == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before it is written again
+            __builtin_amdgcn_sched_barrier(0);
+            if (c0 + step < N) load_w(c0 + step, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         u32x4 o[MT][2];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
             for (int p = 0; p < 2; ++p)
                 if (row[i] >= 0 && col + 8 * p < N) *reinterpret_cast<u32x4*>(out + row[i] * out_ld + (int64_t)(col + 8 * p) * 2) = o[i][p];
         }
-        set ^= 1;
+        set ^= kSets - 1;
     }
 }
 

@@ -302,6 +302,7 @@ def test_captured_and_replayed(e0m4, tokens):
     w1, w2 = make_weights(e0m4, "e0m4", experts, 2 * inner, hidden, 128, 1)[0], make_weights(e0m4, "e0m4", experts, hidden, inner, 128, 2)[0]
     x, logits = torch.zeros((tokens, hidden), dtype=torch.float16, device=DEV), torch.zeros((tokens, experts), device=DEV)
     side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         feed_forward(e0m4, x, logits, k, w1, w2, inner, hidden)
     torch.cuda.synchronize()
