@@ -193,7 +193,8 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
 }
 
 // base + f H B^T for a tile and 64 columns of a wavefront at a time; NT times 16 of the rank.  The row of B in lane (n, q) of the j-th of four
-// MFMAs is column 16 (n/4) + 4 j + n%4, so that a lane's results, 4 q .. + 3 of each, are the columns 16 q .. + 15 of row n.  The 64 rows of B are one piece
+// MFMAs is column 8 (n/4) + 4 (j%2) + 32 (j/2) + n%4, so that a lane's results, 4 q .. + 3 of each, are the columns 8 q .. + 7 and 32 + 8 q .. + 7 of row n and
+// four lanes read and write 64 bytes of it side by side.  The 64 rows of B are one piece
 // of memory that comes to LDS as it is, but for the order of 16-byte pieces in a row (see order_of), one set of columns ahead.  With more than 16 rows the wavefronts make the
 // operands of 16 rows each and share them through LDS.
 __host__ __device__ constexpr int expand_sets(int NT) { return NT >= 4 ? 1 : 2; }
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
     // ---- rows of B: load e brings pieces 64 e .. + 63 of the 64 rows' pieces
     const int ppr = rank / 8;                           // pieces of a row
     const uint32_t reciprocal = small_reciprocal(ppr), adapter_pieces = (uint32_t)N * (uint32_t)ppr;
-    // Where piece p of row 16 a + 4 j + b lies among the row's, a power of two of them: the 16 rows of an operand read (all a and b of a j) fall into different
+    // Where piece p of row 8 a + b (+ 4, + 32) lies among the row's, a power of two of them: the 16 rows of an operand read (all a and b of a j) fall into different
     // bank groups, for two pieces a row into half as many.
     auto order_of = [&](int p, int a, int b) -> int {
         switch (ppr) {
@@ -252,16 +253,16 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
 #pragma unroll
     for (int e = 0; e < 2 * NT; ++e) {
         const uint32_t f = (uint32_t)(e * 64 + lane), r = small_quotient(f, reciprocal), p = f - r * ppr;
-        piece_at[e] = r * ppr + (uint32_t)order_of((int)p, (int)r >> 4, (int)r & 3);
+        piece_at[e] = r * ppr + (uint32_t)order_of((int)p, (int)(r >> 3) & 3, (int)r & 3);
     }
     const __amdgpu_buffer_rsrc_t b_rsrc = make_rsrc(B + (int64_t)tile.group * N * rank * 2);
     constexpr int kSets = expand_sets(NT);
     unsigned char* w_lds = smem + (kShared ? NT * MT * 1024 + MT * 64 : 0) + wave * (kSets * 64 * NT * 32);
-    uint32_t w_at[NT];                                  // of step j, MFMA 0 (a row of MFMA j4: 4 j4 rows on); the rank's end: any piece, its operand is zeroed
+    uint32_t w_at[NT];                                  // of step j, MFMA 0; the rank's end: any piece, its operand is zeroed
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int p = 2 * j + (q & 1);
-        w_at[j] = (uint32_t)((16 * (n_l >> 2) + (n_l & 3)) * rank * 2 + order_of(p < ppr ? p : 0, n_l >> 2, n_l & 3) * 16);
+        w_at[j] = (uint32_t)((8 * (n_l >> 2) + (n_l & 3)) * rank * 2 + order_of(p < ppr ? p : 0, n_l >> 2, n_l & 3) * 16);
     }
     auto load_w = [&](int at, int set) {
 #pragma unroll
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                const int col = at + 16 * q + 8 * p;
+                const int col = at + 8 * q + 32 * p;
                 b[i][p] = u32x4{0, 0, 0, 0};
                 if (base && row[i] >= 0 && col < N) b[i][p] = *reinterpret_cast<const u32x4*>(base + row[i] * base_ld + (int64_t)col * 2);
             }
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
         __builtin_amdgcn_sched_barrier(0);
         if (kSets == 2 && c0 + step < N) load_w(c0 + step, set ^ 1);
         __builtin_amdgcn_sched_barrier(0);
-        const int col = c0 + 16 * q;                    // this lane's results: columns col .. col + 15 of its rows
+        const int col = c0 + 8 * q;                     // this lane's results: columns col .. + 7 and col + 32 .. + 7 of its rows
         floatx4 acc[4][MT];
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4)
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
             half8_t w[4];
 #pragma unroll
             for (int j4 = 0; j4 < 4; ++j4) {
-                w[j4] = *reinterpret_cast<const half8_t*>(w_lds + set * (64 * NT * 32) + w_at[j] + 4 * j4 * rank * 2);
+                w[j4] = *reinterpret_cast<const half8_t*>(w_lds + set * (64 * NT * 32) + w_at[j] + (4 * (j4 & 1) + 32 * (j4 >> 1)) * rank * 2);
                 if (2 * j + (q & 1) >= ppr) w[j4] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
             }
 #pragma unroll
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
             for (int p = 0; p < 2; ++p)
-                if (row[i] >= 0 && col + 8 * p < N) *reinterpret_cast<u32x4*>(out + row[i] * out_ld + (int64_t)(col + 8 * p) * 2) = o[i][p];
+                if (row[i] >= 0 && col + 32 * p < N) *reinterpret_cast<u32x4*>(out + row[i] * out_ld + (int64_t)(col + 32 * p) * 2) = o[i][p];
         }
         set ^= kSets - 1;
     }
