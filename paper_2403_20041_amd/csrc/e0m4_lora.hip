@@ -4,10 +4,11 @@
 // in turn, read rows of X and of A as the matrix cores take them and add their sums in LDS; few tiles are split along K over workgroups,
 // each with a slab of its own.  The second, out = base + f H B^T: H is added up over the slabs in order and split into the sum of two 16-bit numbers (fp16
 // after scaling its row by a power of two: 22 bits, bfloat16: 16), so that its rounding is far below that of the output; a wavefront has the rows of
-// the tile and 64 columns at a time, of which a lane holds 16 neighbours of one row.
+// the tile and 64 columns at a time, of which a lane holds two runs of 8 of one row.
 // What bounds it: memory, X once, base and out once, A and B of the adapters in use once (and from L2 for every further tile).  3001 rows of five
 // requests, rank 64, 4096 x 4096: 9 - 10 us and 16 - 19 of a floor of 16 together (A comes from L2 94 times, base and out pass through registers of few
-// wavefronts); 8192 rows of rank 16 43 of 41; 64 rows with 40 adapters of rank 16 3.5 and 5.4 us, two launches' chains of loads.
+// wavefronts); 8192 rows of rank 16 41 of 41, of rank 64 65 of 42; 5253 rows of rank 16, 15832 x 7672 128 of 84; 64 rows with 40 adapters of rank 16 3.5 and 5.4 us,
+// two launches' chains of loads, of rank 128 30 of 14.
 #include "e0m4_groups.h"
 
 #include <algorithm>
@@ -195,8 +196,9 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
 // base + f H B^T for a tile and 64 columns of a wavefront at a time; NT times 16 of the rank.  The row of B in lane (n, q) of the j-th of four
 // MFMAs is column 8 (n/4) + 4 (j%2) + 32 (j/2) + n%4, so that a lane's results, 4 q .. + 3 of each, are the columns 8 q .. + 7 and 32 + 8 q .. + 7 of row n and
 // four lanes read and write 64 bytes of it side by side.  The 64 rows of B are one piece
-// of memory that comes to LDS as it is, but for the order of 16-byte pieces in a row (see order_of), one set of columns ahead.  With more than 16 rows the wavefronts make the
-// operands of 16 rows each and share them through LDS.
+// of memory that comes to LDS as it is, but for the order of 16-byte pieces in a row (see order_of): up to a rank of 48 one set of columns ahead; beyond, into the same LDS
+// once its operands are in registers, which leaves room for more workgroups of a compute unit (64 rows of 40 adapters of rank 128: 39 us with two sets, 30 with one).
+// With more than 16 rows the wavefronts make the operands of 16 rows each and share them through LDS.
 __host__ __device__ constexpr int expand_sets(int NT) { return NT >= 4 ? 1 : 2; }
 __host__ __device__ constexpr int expand_lds(int MT, int NT) { return (MT > 1 ? NT * MT * 1024 + MT * 64 : 0) + kWavesL * expand_sets(NT) * 64 * NT * 32; }
 template <bool BF, int MT, int NT>
@@ -374,7 +376,9 @@ struct LoraPlan {
 // no more rows.  3001 rows of five requests, rank 64, 4096 x 4096, both launches, in us (rows of a tile in the first / second launch, splits, workgroups per tile in the
 // second): 16/16 1 4 39.0, 16/32 1 4 30.7, 32/32 2 4 30.5, 32/64 2 4 32.9, 64/32 2 4 33.4, 16/32 1 16 34.3; 512 rows of two, rank 32: 16/16 2 11.7, 16/32 2 11.1, 4 11.5,
 // 8 13.4, 32/32 2 12.4; 64 rows of 40 adapters, rank 16: 1, 2, 4 and 8 splits 9.6, 8.6, 8.4, 9.1; 8192 rows of four, rank 16: 16/32 1 with 2 and 4
-// workgroups per tile 45.4 and 42.5, 32/32 46.5.
+// workgroups per tile 45.4 and 42.5, 32/32 46.5.  Workgroups of the second launch: a rank of 32 or less has little to bring before its first column, and 1024 against 2048
+// took 43.3 and 40.8 (8192 rows of four, rank 16) and 136 and 128 (5253 of one, rank 16, 15832 x 7672); beyond that 448 against 896 took 30 and 35 (3001 rows, rank 64),
+// 98 and 103 (4671 of 67, rank 128, 8008 x 2576), 65 and 63 (8192, rank 64).
 LoraPlan plan_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
 {
     LoraPlan p;
@@ -385,7 +389,7 @@ LoraPlan plan_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t 
     p.expand_tiles = most_tiles(rows, adapters, tile_height(p.expand_height));
     const int64_t chunks = (K + kChunkK - 1) / kChunkK;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / p.shrink_tiles, (chunks + kWavesL - 1) / kWavesL, 4}));
-    const int64_t parts = (N + kWavesL * 64 - 1) / (kWavesL * 64), workgroups = rank > 32 ? 448 : 1024;
+    const int64_t parts = (N + kWavesL * 64 - 1) / (kWavesL * 64), workgroups = rank > 32 ? 448 : 2048;
     p.columns = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(parts, (workgroups + p.expand_tiles - 1) / p.expand_tiles));
     return p;
 }
