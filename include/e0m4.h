@@ -534,7 +534,8 @@ int e0m4_bf16_matmul_grouped(const void* X_bf16, int64_t share, const void* plan
 /*
  * out[t, n] = base[t, n] + sum_j weights[t, j] * Y[place[t * k + j], n] over the entries j
  * < k that have a place, added up in fp32 in that order and rounded once.  Y is
- * [tokens * k, N] as e0m4_matmul_grouped leaves it, base (NULL: zeros) and out [tokens, N], fp16 or bf16; out may be base.
+ * [tokens * k, N] as e0m4_matmul_grouped leaves it, base (NULL: zeros) and out [tokens, N], fp16 or bf16; out may be base, and overlaps
+ * nothing else.
  */
 int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, const void* plan, int64_t tokens, int k, int64_t groups, const void* base,
                  void* out, void* stream);
@@ -545,7 +546,7 @@ int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, cons
  * the other rows keep their base.  The layout's entries are the rows, its groups the adapters.  X is [rows, K], base
  * and out [rows, N], rows x_ld, base_ld and out_ld elements apart; A [adapters, rank, K], B [adapters, N, rank], all
  * fp16 or bf16; factors fp32 [adapters] (NULL: ones).  base may be NULL (zeros) or out, with the same distance of rows; otherwise
- * they do not overlap.  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
+ * their rows do not overlap (both may be columns of one wider matrix).  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
  * distances multiples of 8, N <= 2^24, K <= 2^20, X and one adapter's B less than 2 GiB.  A X is accumulated in fp32 and multiplied in two 16-bit
  * parts (22 bits of each row's largest, bf16: 16), the sum with base is rounded once.  Workspace as for e0m4_matmul.
  */

@@ -14,6 +14,15 @@ bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
     const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
     return p < q + b_bytes && q < p + a_bytes;
 }
+// Rows of `bytes`, a_ld and b_ld bytes apart.  Columns of one wider matrix lie between each other without touching.
+bool rows_overlap(const void* a, int64_t a_ld, const void* b, int64_t b_ld, int64_t rows, int64_t bytes)
+{
+    if (!overlap(a, (size_t)((rows - 1) * a_ld + bytes), b, (size_t)((rows - 1) * b_ld + bytes))) return false;
+    if (a_ld != b_ld) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    const int64_t apart = (int64_t)((p > q ? p - q : q - p) % (uintptr_t)a_ld);
+    return apart < bytes || apart > a_ld - bytes;
+}
 
 int check_groups(int64_t rows, int64_t groups)
 {
@@ -98,6 +107,8 @@ int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows,
     if (rows == 0 || N == 0) return E0M4_OK;
     if (!X || !plan || !codes || !Y) return E0M4_ERR_NULL;
     if (!aligned(X, 16) || !aligned(plan, 16) || !aligned(codes, 16) || !aligned(Y, 16)) return E0M4_ERR_ALIGN;
+    const int64_t n_out = epilogue == E0M4_EPILOGUE_SWIGLU ? N / 2 : N;
+    if (overlap(X, (size_t)(share ? rows / share : rows) * K * 2, Y, (size_t)rows * n_out * 2)) return E0M4_ERR_SHAPE;
     GroupedArgs a;
     a.X = X;
     a.share = share;
@@ -232,6 +243,7 @@ int e0m4_lora(const void* X, int64_t x_ld, int dtype, const void* plan, int64_t 
         !aligned(workspace, 16))
         return E0M4_ERR_ALIGN;
     if (((rows - 1) * x_ld + K) * 2 > kMaxXBytes) return E0M4_ERR_SHAPE;
+    if (base && base != out && rows_overlap(base, base_ld * 2, out, out_ld * 2, rows, N * 2)) return E0M4_ERR_SHAPE;
     if (workspace_bytes < lora_workspace_bytes(rows, adapters, rank, N, K)) return E0M4_ERR_WORKSPACE;
     LoraArgs a;
     a.X = X;

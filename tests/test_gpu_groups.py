@@ -265,6 +265,25 @@ def test_lora(e0m4, dtype, rows, adapters, rank, N, K, runs):
     assert not got.cpu()[none].any()
 
 
+@pytest.mark.parametrize("rows", [1, 70])
+def test_lora_between_columns_of_one_matrix(e0m4, rows):
+    """base and out beside each other in the rows of one matrix: the columns around out keep what they were."""
+    adapters, rank, N, K = 2, 16, 72, 136
+    g = gen(rows)
+    index = torch.randint(-1, adapters, (rows,), generator=g, dtype=torch.int32)
+    X = torch.randn((rows, K), generator=g).half().to(DEV)
+    A, B = torch.randn((adapters, rank, K), generator=g).half().to(DEV), torch.randn((adapters, N, rank), generator=g).half().to(DEV)
+    wide = torch.randn((rows, 2 * N + 8), generator=g).half().to(DEV)
+    plan = e0m4.e0m4_groups(index.to(DEV), adapters)
+    want = e0m4.e0m4_lora(X, plan, A, B, base=wide[:, :N].clone())
+    before = wide.clone()
+    e0m4.e0m4_lora(X, plan, A, B, base=wide[:, :N], out=wide[:, N:2 * N])
+    assert torch.equal(wide[:, N:2 * N], want)
+    assert torch.equal(wide[:, :N], before[:, :N]) and torch.equal(wide[:, 2 * N:], before[:, 2 * N:])
+    with pytest.raises(RuntimeError):
+        e0m4.e0m4_lora(X, plan, A, B, base=wide[:, :N], out=wide[:, N - 8:2 * N - 8])
+
+
 def test_lora_of_large_small_and_infinite_rows(e0m4):
     """fp16: A x far outside fp16's range, below it, zero, and rows that hold NaN or an infinity."""
     K, N, rank = 64, 64, 16

@@ -73,6 +73,15 @@ def test_products_refuse(L, name, groups):
     assert call(rows=0, X=None, Y=None) == 0 and call(N=0) == 0
 
 
+@pytest.mark.parametrize("name", ["e0m4_matmul_grouped", "e0m4_bf16_matmul_grouped", "e0m8_matmul_grouped"])
+@pytest.mark.parametrize("share,epilogue", [(0, 0), (2, 0), (0, 1)])
+def test_products_refuse_results_over_their_rows(L, name, share, epilogue):
+    rows, N, K, far = 8, 128, 256, 1 << 40
+    x_bytes, y_bytes = (rows // share if share else rows) * K * 2, rows * (N // 2 if epilogue else N) * 2
+    for y in (far, far + x_bytes - 16, far - y_bytes + 16):
+        assert getattr(L, name)(ctypes.c_void_p(far), share, P, rows, 4, P, N, K, 128, epilogue, ctypes.c_void_p(y), None) == SHAPE, y - far
+
+
 def test_combine_refuses(L):
     def call(Y=P, dtype=0, N=64, weights=P, plan=P, tokens=4, k=2, groups=8, base=None, out=FAR):
         return L.e0m4_combine(Y, dtype, N, weights, plan, tokens, k, groups, base, out, None)
@@ -103,6 +112,15 @@ def test_lora_refuses(L):
                 dict(factors=ctypes.c_void_p(0x10002))):
         assert call(**bad) == ALIGN, bad
     assert call(ws_bytes=L.e0m4_lora_workspace_bytes(4, 3, 16, 128, 256) - 1) == WORKSPACE
+    # results over other rows or columns of base; columns beside each other go on to the next check
+    few = dict(ws_bytes=0)
+    at = lambda columns: ctypes.c_void_p((1 << 40) + 2 * columns)  # noqa: E731
+    for bad in (dict(base=at(8)), dict(base=at(128)), dict(base=at(-8)), dict(base=at(3 * 128 + 120)), dict(base=at(120), base_ld=256, out_ld=256),
+                dict(base=at(136), base_ld=256, out_ld=256), dict(base=at(256), base_ld=256, out_ld=256), dict(base=at(128), base_ld=256, out_ld=264)):
+        assert call(**bad, **few) == SHAPE, bad
+    for good in (dict(base=at(128), base_ld=256, out_ld=256), dict(base=at(-128), base_ld=256, out_ld=256), dict(base=at(4 * 128)), dict(base=at(-4 * 128)),
+                 dict(base=at(0)), dict(base=at(128), base_ld=264, out_ld=264)):
+        assert call(**good, **few) == WORKSPACE, good
     assert call(rows=0, X=None, ws=None) == 0 and call(N=0) == 0
 
 
