@@ -63,7 +63,13 @@ def test_adapters_beside_the_output_projection(e0m4):
         blocks[0](torch.zeros((batch, 1, hidden), dtype=torch.float16, device="cuda"), adapter=adapter)
     with pytest.raises(ValueError):
         blocks[0].add_adapters(A, B[:, :-8])
+    for bad in ((A.bfloat16(), B.bfloat16()), (A.cpu(), B), (A, B, factors.half()), (A, B, factors[:1]), (A[:, :4].contiguous(), B[..., :4].contiguous())):
+        with pytest.raises(ValueError):
+            blocks[0].add_adapters(*bad)
     blocks[0].add_adapters(A, B, factors)
+    with pytest.raises(ValueError):                             # refused before rows are appended
+        blocks[0](torch.zeros((batch, 1, hidden), dtype=torch.float16, device="cuda"), adapter=adapter.cpu())
+    assert blocks[0].most == 0
     for n in (20, 1, 1):
         x = torch.randn((batch, n, hidden), generator=g).half().cuda()
         with_, without = blocks[0](x, adapter=adapter), blocks[1](x)
