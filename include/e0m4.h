@@ -547,8 +547,9 @@ int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, cons
  * and out [rows, N], rows x_ld, base_ld and out_ld elements apart; A [adapters, rank, K], B [adapters, N, rank], all
  * fp16 or bf16; factors fp32 [adapters] (NULL: ones).  base may be NULL (zeros) or out, with the same distance of rows; otherwise
  * their rows do not overlap (both may be columns of one wider matrix).  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
- * distances multiples of 8, N <= 2^24, K <= 2^20, X and one adapter's B less than 2 GiB.  A X is accumulated in fp32 and multiplied in two 16-bit
- * parts (22 bits of each row's largest, bf16: 16), the sum with base is rounded once.  Workspace as for e0m4_matmul.
+ * distances multiples of 8, N <= 2^24, K <= 2^20, X and one adapter's B less than 2 GiB.  A X is accumulated in fp32 and multiplied
+ * with all its bits (fp16: down to 2^-38 of its row's largest), the sum with base is rounded once.  An infinity in A X or B may give NaN.
+ * Workspace as for e0m4_matmul.
  */
 size_t e0m4_lora_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K);
 int e0m4_lora(const void* X, int64_t x_ld, int dtype, const void* plan, int64_t rows, int64_t adapters, const void* A, const void* B, int rank,

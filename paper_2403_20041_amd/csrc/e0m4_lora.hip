@@ -2,8 +2,8 @@
 //
 // Two launches over tiles of rows of one adapter (see e0m4_groups.h).  The first, H = X A^T: a workgroup's four wavefronts take 128-k chunks
 // in turn, read rows of X and of A as the matrix cores take them and add their sums in LDS; few tiles are split along K over workgroups,
-// each with a slab of its own.  The second, out = base + f H B^T: H is added up over the slabs in order and split into the sum of two 16-bit numbers (fp16
-// after scaling its row by a power of two: 22 bits, bfloat16: 16), so that its rounding is far below that of the output; a wavefront has the rows of
+// each with a slab of its own.  The second, out = base + f H B^T: H is added up over the slabs in order and split into the sum of three 16-bit numbers (fp16
+// after scaling its row by a power of two), which hold all 24 bits of it: nothing is rounded between the two products.  A wavefront has the rows of
 // the tile and 64 columns at a time, of which a lane holds two runs of 8 of one row.
 // What bounds it: memory, X once, base and out once, A and B of the adapters in use once (and from L2 for every further tile).  3001 rows of five
 // requests, rank 64, 4096 x 4096: 9 - 10 us and 16 - 19 of a floor of 16 together (A comes from L2 94 times, base and out pass through registers of few
@@ -139,10 +139,14 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_shrink_kernel(const void* p
     }
 }
 
-// 16 rows of H as operands of the expanding product, NT times 16 of the rank, and what their product is to be multiplied with: the 32 values
-// of "k" of an operand are 16 of the rank as their upper parts (q 0, 1), then the same as the lower parts (q 2, 3).
+// 16 rows of H as operands of the expanding product, NT times 16 of the rank, and what their product is to be multiplied with.  H is the sum of three 16-bit
+// parts: each is what the ones before it left, rounded, and what it leaves is exact in fp32.  An operand's 32 values of "k" are 16 of the rank for two parts, the
+// first (q 0, 1) and the second (q 2, 3), or the third and zeros.  (Two parts leave 16 of bfloat16's 24 bits: 415 rows of rank 128 have 2.3e-3 of the results rounded
+// the other way than the exact sums, 1.9e-4 with three; fp32 operands have 3.6e-4.  The third one costs 30.0 -> 31.5 us with 3001 rows of rank 64, 4096 x 4096, 148 -> 158
+// with 4671 of rank 128, 8008 x 2576, 42.3 -> 42.5 with 8192 of rank 16.)
+constexpr int kPartPairs = 2;
 template <bool BF, int NT>
-__device__ inline void split_rows(const float* H, bool in, int rank, int splits, int64_t slab, float factor, int q, half8_t (&h)[NT], float& scale)
+__device__ inline void split_rows(const float* H, bool in, int rank, int splits, int64_t slab, float factor, int q, half8_t (&h)[kPartPairs][NT], float& scale)
 {
     typedef std::conditional_t<BF, __bf16, half_t> T;
     typedef T T8 __attribute__((ext_vector_type(8)));
@@ -163,9 +167,10 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
             v[j][4 + e] = hi[e];
         }
     }
-    // fp16: the row's largest magnitude is scaled into [1/2, 1) (powers of two: exact).  A row that holds an infinity or NaN is used as it is.
+    // fp16: the row's largest magnitude is scaled into [2^14, 2^15) (powers of two: exact), so that what is 2^-15 of it still has all its bits above the least
+    // number of the type, 2^-24, and what is 2^-28 of it eleven.  A row that holds an infinity is used as it is; NaN (which the maximum passes over) stays NaN.
     scale = factor;
-    float down = 1.f;
+    float up = 1.f;
     if constexpr (!BF) {
         float most = 0.f;
 #pragma unroll
@@ -174,22 +179,25 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
             for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[j][e]));
         most = fmaxf(most, __shfl_xor(most, 16));
         if (most > 0.f && most < INFINITY) {
-            const int exponent = min(max(__builtin_amdgcn_frexp_expf(most), -126), 126);
-            down = __builtin_amdgcn_ldexpf(1.f, -exponent);
+            const int exponent = min(max(__builtin_amdgcn_frexp_expf(most) - 15, -126), 126);
+            up = __builtin_amdgcn_ldexpf(1.f, -exponent);
             scale = factor * __builtin_amdgcn_ldexpf(1.f, exponent);
         }
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        T8 part16;
+        T8 pair[kPartPairs];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = v[j][e] * down;
-            const T upper = (T)x;
-            const float rest = x - (float)upper;
-            part16[e] = q < 2 ? upper : fabsf((float)upper) < INFINITY ? (T)rest : (T)0.f;
+            const float x = v[j][e] * up;
+            const T first = (T)x;
+            const float rest = fabsf((float)first) < INFINITY ? x - (float)first : 0.f;     // (NaN, too, is in the first part alone)
+            const T second = (T)rest;
+            pair[0][e] = q < 2 ? first : second;
+            pair[1][e] = q < 2 ? (T)(rest - (float)second) : (T)0.f;
         }
-        h[j] = __builtin_bit_cast(half8_t, part16);
+#pragma unroll
+        for (int p = 0; p < kPartPairs; ++p) h[p][j] = __builtin_bit_cast(half8_t, pair[p]);
     }
 }
 
@@ -200,7 +208,8 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
 // once its operands are in registers, which leaves room for more workgroups of a compute unit (64 rows of 40 adapters of rank 128: 39 us with two sets, 30 with one).
 // With more than 16 rows the wavefronts make the operands of 16 rows each and share them through LDS.
 __host__ __device__ constexpr int expand_sets(int NT) { return NT >= 4 ? 1 : 2; }
-__host__ __device__ constexpr int expand_lds(int MT, int NT) { return (MT > 1 ? NT * MT * 1024 + MT * 64 : 0) + kWavesL * expand_sets(NT) * 64 * NT * 32; }
+__host__ __device__ constexpr int operand_lds(int MT, int NT) { return MT > 1 ? kPartPairs * NT * MT * 1024 + MT * 64 : 0; }
+__host__ __device__ constexpr int expand_lds(int MT, int NT) { return operand_lds(MT, NT) + kWavesL * expand_sets(NT) * 64 * NT * 32; }
 template <bool BF, int MT, int NT>
 __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* plan, int rows, int adapters, uint32_t columns, uint32_t tile_grid, const float* H, int rank,
                                                                     int splits, const char* B, const float* factors, int N, const char* base, char* out,
@@ -211,8 +220,8 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
     constexpr int HEIGHT = MT - 1;
     constexpr bool kShared = MT > 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    half8_t* operands = reinterpret_cast<half8_t*>(smem);                               // [NT][MT][64]
-    float* scales = reinterpret_cast<float*>(smem + NT * MT * 1024);                    // [MT * 16]
+    half8_t* operands = reinterpret_cast<half8_t*>(smem);                               // [pairs of parts][NT][MT][64]
+    float* scales = reinterpret_cast<float*>(smem + kPartPairs * NT * MT * 1024);       // [MT * 16]
     const GroupPlan lay = plan_view(plan, rows, adapters);
     const int lane = threadIdx.x & 63, n_l = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -259,7 +268,7 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
     }
     const __amdgpu_buffer_rsrc_t b_rsrc = make_rsrc(B + (int64_t)tile.group * N * rank * 2);
     constexpr int kSets = expand_sets(NT);
-    unsigned char* w_lds = smem + (kShared ? NT * MT * 1024 + MT * 64 : 0) + wave * (kSets * 64 * NT * 32);
+    unsigned char* w_lds = smem + operand_lds(MT, NT) + wave * (kSets * 64 * NT * 32);
     uint32_t w_at[NT];                                  // of step j, MFMA 0; the rank's end: any piece, its operand is zeroed
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -294,14 +303,16 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
             }
     };
     load_base(c0);
-    half8_t mine[NT];
+    half8_t mine[kPartPairs][NT];
     float scale[MT];
     if constexpr (kShared) {
         if (wave < MT) {
             const int m = 16 * wave + n_l;
             split_rows<BF, NT>(H + (int64_t)(first + m) * rank, m < M, rank, splits, slab, factor, q, mine, scale[0]);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) operands[(j * MT + wave) * 64 + lane] = mine[j];
+            for (int p = 0; p < kPartPairs; ++p)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) operands[((p * NT + j) * MT + wave) * 64 + lane] = mine[p][j];
             if (q == 0) scales[m] = scale[0];
         }
         __syncthreads();
@@ -332,9 +343,12 @@ __global__ __launch_bounds__(kThreadsL, 2) void lora_expand_kernel(const void* p
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const half8_t h = kShared ? operands[(j * MT + i) * 64 + lane] : mine[j];
 #pragma unroll
-                for (int j4 = 0; j4 < 4; ++j4) acc[j4][i] = mfma16<BF>(w[j4], h, acc[j4][i]);
+                for (int p = 0; p < kPartPairs; ++p) {
+                    const half8_t h = kShared ? operands[((p * NT + j) * MT + i) * 64 + lane] : mine[p][j];
+#pragma unroll
+                    for (int j4 = 0; j4 < 4; ++j4) acc[j4][i] = mfma16<BF>(w[j4], h, acc[j4][i]);
+                }
             }
         }
         if (kSets == 1) {
