@@ -521,8 +521,9 @@ int e0m4_route(const void* logits, int dtype, int64_t tokens, int64_t experts, i
  * (e0m8_codes_bytes) bytes.  N <= 2^24, 0 < K, K as for e0m4_matmul (e0m8_matmul), with
  * share > 0 X of less than 2 GiB, gated the gate's half of a buffer of at most 1 GiB.
  * Accumulation is fp32; every weight is rounded to 16 bits as the dequant entry points do.  Y may not
- * overlap X.  No workspace.  A call whose tiles times column blocks would not fit one launch (2^32
- * work items, more than 3e11 outputs) is refused (E0M4_ERR_SHAPE).
+ * overlap X.  No workspace.  A call is one launch, with work for rows / 128 + min(rows, groups) tiles times
+ * N / 256 (rounded up) blocks of columns, whether tiles are full or not: more than 2^24 - 64 of them do not
+ * fit and may be refused (E0M4_ERR_SHAPE).
  */
 int e0m4_matmul_grouped(const void* X_f16, int64_t share, const void* plan, int64_t rows, int64_t groups, const void* codes, int64_t N, int64_t K,
                         int group, int epilogue, void* Y_f16, void* stream);

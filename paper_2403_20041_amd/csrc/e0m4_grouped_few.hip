@@ -276,15 +276,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(const char*
 }
 
 template <int FMT, int MT, int R, bool GATED>
-int launch_few(const FewArgs& f, int64_t tiles, hipStream_t stream)
+int launch_few(const FewArgs& f, hipStream_t stream)
 {
     constexpr int lds = std::max(kFewWaves * R * MT * 64 * 16, kFewWaves * MT * 16 * (FMT == kGroupedE8 ? 128 : 256));
     FewArgs a = f;
     const uint32_t blocks = GATED ? a.N / 2 / kBlockRows : (uint32_t)row_blocks(a.N);
     constexpr uint32_t RH = GATED ? R / 2 : R;
     a.chunks = (blocks + RH - 1) / RH;
-    const int64_t grid = tiles * a.chunks;
-    if (grid * kFewThreads > 0xffffffffLL) return E0M4_ERR_SHAPE;
+    const int64_t grid = grouped_workgroups(a.rows, a.groups, 16 * MT, a.chunks);
+    if (grid * kFewThreads > kMaxWorkItems) return E0M4_ERR_SHAPE;
     static std::atomic<uint64_t> lds_allowed{0};
     const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_few_kernel<FMT, MT, R, GATED>), lds, lds_allowed);
     if (rc != E0M4_OK) return rc;
@@ -294,11 +294,11 @@ int launch_few(const FewArgs& f, int64_t tiles, hipStream_t stream)
 }
 
 template <int FMT, bool GATED>
-int launch_few_as(const FewArgs& f, int64_t tiles, int height, int row_blocks, hipStream_t stream)
+int launch_few_as(const FewArgs& f, int height, int row_blocks, hipStream_t stream)
 {
-    if (height == 32 && row_blocks == 4) return launch_few<FMT, 2, 4, GATED>(f, tiles, stream);
-    if (height == 16 && row_blocks == 4) return launch_few<FMT, 1, 4, GATED>(f, tiles, stream);
-    if (height == 16 && row_blocks == 2) return launch_few<FMT, 1, 2, GATED>(f, tiles, stream);
+    if (height == 32 && row_blocks == 4) return launch_few<FMT, 2, 4, GATED>(f, stream);
+    if (height == 16 && row_blocks == 4) return launch_few<FMT, 1, 4, GATED>(f, stream);
+    if (height == 16 && row_blocks == 2) return launch_few<FMT, 1, 2, GATED>(f, stream);
     return E0M4_ERR_SHAPE;
 }
 
@@ -318,11 +318,9 @@ int launch_grouped_few(const GroupedArgs& a, int format, int height, int row_blo
     f.chunks = 0;
     f.kind = (uint32_t)a.share << 4 | (format == kGroupedE8 || a.group == 128 ? 7 : a.group == 64 ? 6 : 5);
     f.share_reciprocal = small_reciprocal(a.share);
-    const int64_t tiles = most_tiles(a.rows, a.groups, height);
     auto go = [&](auto fmt_c) -> int {
         constexpr int FMT = decltype(fmt_c)::value;
-        return a.swiglu ? launch_few_as<FMT, true>(f, tiles, height, row_blocks, stream)
-                        : launch_few_as<FMT, false>(f, tiles, height, row_blocks, stream);
+        return a.swiglu ? launch_few_as<FMT, true>(f, height, row_blocks, stream) : launch_few_as<FMT, false>(f, height, row_blocks, stream);
     };
     switch (format) {
         case kGroupedFp16: return go(std::integral_constant<int, kGroupedFp16>{});

@@ -31,7 +31,6 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr int BK = 64;
 constexpr int kRowBytes = BK * 2, kStages = 4;
-constexpr int kNumXcd = 8;
 constexpr int TN = 2;                           // operand blocks of 32 weight rows per wavefront
 
 // (as kernel arguments one by one, in registers from the start)
@@ -443,8 +442,8 @@ int launch_many(const ManyArgs& f, int64_t rows, int64_t groups, hipStream_t str
     ManyArgs a = f;
     const int64_t columns = GATED ? 32 * WN : 64 * WN, n_out = GATED ? a.N / 2 : a.N;
     a.n_tiles = (uint32_t)((n_out + columns - 1) / columns);
-    const int64_t grid = (most_tiles(rows, groups, 32 * TM) * a.n_tiles / kNumXcd + kTileClasses) * kNumXcd;
-    if (grid * threads > 0xffffffffLL) return E0M4_ERR_SHAPE;
+    const int64_t grid = grouped_workgroups(rows, groups, 32 * TM, a.n_tiles);
+    if (grid * threads > kMaxWorkItems) return E0M4_ERR_SHAPE;
     static std::atomic<uint64_t> lds_allowed{0};
     const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&grouped_many_kernel<FMT, G, GATED, TM, WN, KS>), lds, lds_allowed);
     if (rc != E0M4_OK) return rc;

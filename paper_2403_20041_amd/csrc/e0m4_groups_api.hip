@@ -76,22 +76,25 @@ constexpr GroupedForm kGroupedForms[] = {
     {128, 128, 2, 3.982, 0.7367, 0.0077, 0.9139, 0.0105, 2.610, 1.149, 1.131, 1.101, 1.319},
 };
 constexpr int kGroupedFormCount = sizeof(kGroupedForms) / sizeof(kGroupedForms[0]);
+constexpr int kFewestWorkItems = 3;
 
 const GroupedForm& choose_form(int64_t rows, int64_t groups, int64_t N, int64_t K, bool gated, int format)
 {
     const int force = knob(Knob::grouped_form);
     if (force >= 1 && force <= kGroupedFormCount) return kGroupedForms[force - 1];
     const double used = fmax(1.0, groups * (1.0 - exp(-(double)rows / groups)));
-    const GroupedForm* best = kGroupedForms;
-    double least = 0;
+    const GroupedForm* best = &kGroupedForms[kFewestWorkItems];      // (which refuses the call if no form's grid has room for it)
+    double least = INFINITY;
     for (const GroupedForm& f : kGroupedForms) {
-        const int64_t columns = gated ? f.columns / 2 : f.columns, out = gated ? N / 2 : N;
-        const double tiles = fmax(used, rows / (double)f.height + 0.5 * used), w = tiles * ((out + columns - 1) / columns) / 256;
+        const int64_t columns = gated ? f.columns / 2 : f.columns, out = gated ? N / 2 : N, blocks = (out + columns - 1) / columns;
+        const int64_t threads = f.height < 64 ? 64 * f.parts : f.columns * f.parts;
+        if (grouped_workgroups(rows, groups, f.height, blocks) * threads > kMaxWorkItems) continue;
+        const double tiles = fmax(used, rows / (double)f.height + 0.5 * used), w = tiles * blocks / 256;
         const double one = format == kGroupedBf16 ? f.one_bf16 : format == kGroupedE8 ? f.one_e8 : 1.0;
         const double full = format == kGroupedBf16 ? f.full_bf16 : format == kGroupedE8 ? f.full_e8 : 1.0;
         const double r = rows / tiles, b = K / 128.0 / f.parts;
         const double us = f.start + b * fmax((f.one + f.one_row * r) * one, (f.full + f.full_row * r) * w * full) + f.each * w;
-        if (&f == kGroupedForms || us < least) {
+        if (us < least) {
             least = us;
             best = &f;
         }
