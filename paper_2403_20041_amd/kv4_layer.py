@@ -44,8 +44,8 @@ class Kv4AttentionBlock:
         if A.dim() != 3 or B.shape != (A.shape[0], self.hidden, A.shape[1]) or A.shape[2] != self.hidden:
             raise ValueError("A must be [adapters, rank, %d] and B [adapters, %d, rank], got %s and %s" % (self.hidden, self.hidden, tuple(A.shape), tuple(B.shape)))
         device = self.gamma.device
-        if any(t.dtype != torch.float16 or t.device != device or not t.is_contiguous() for t in (A, B)):
-            raise ValueError("A and B must be contiguous float16 tensors on %s" % device)
+        if any(t.dtype != torch.float16 or t.device != device or not t.is_contiguous() or t.data_ptr() % 16 for t in (A, B)):
+            raise ValueError("A and B must be contiguous float16 tensors on %s that begin at a multiple of 16 bytes" % device)
         if factors is not None and (factors.dtype != torch.float32 or factors.shape != A.shape[:1] or factors.device != device or not factors.is_contiguous()):
             raise ValueError("factors must be float32 [%d] on %s" % (A.shape[0], device))
         if e0m4.e0m4_lora_workspace_bytes(1, A.shape[0], A.shape[1], self.hidden, self.hidden) == 0:
@@ -73,6 +73,8 @@ class Kv4AttentionBlock:
         if adapter is not None and (self.adapters is None or adapter.shape != (batch,) or adapter.dtype != torch.int32 or
                                     adapter.device != x.device):
             raise ValueError("adapter must be int32 [%d] on the block's device, for a block that has adapters" % batch)
+        if adapter is not None and batch * n * hidden * 2 >= 1 << 31:
+            raise ValueError("%d rows of %d are more than e0m4_lora takes (2 GiB)" % (batch * n, hidden))
         flat = x.reshape(batch * n, hidden)
         qkv = e0m4.e0m4_matmul_fused(flat, self.qkv, self.columns, hidden, self.group, rms_gamma=self.gamma, rms_eps=1e-5)
         if self.most + n > self.shape.capacity:
