@@ -481,6 +481,11 @@ int e0m4_kv4_evict(const void* cache, const e0m4_kv4_shape* shape, const float* 
  *       place [rows]          where each entry is in `order`, -1 for those of no group
  *     and goes on with what the library keeps for itself.  It is read by calls that
  *     name the same rows and groups, and free for reuse once these have completed.
+ *     Kernels go where it says, and no call can look at it on the host: it must have been
+ *     written, by e0m4_groups or e0m4_route with the same rows and groups, before them in
+ *     stream order (on another stream: behind an event or a synchronisation), and it
+ *     overlaps nothing else that a call is given.  (In memory of zeros no group has entries, and
+ *     nothing is reached out of range.)
  * Errors, streams and empty problems are as elsewhere in this file, results are
  * deterministic.
  */

@@ -550,12 +550,22 @@ def e0m4_groups_bytes(rows: int, groups: int) -> int:
     return _groups_bytes(rows, groups)
 
 
-def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups:
-    """Memory for the layout of `rows` entries by `groups` weights (uninitialised)."""
+def _new_groups(rows: int, groups: int, device, stream) -> E0M4Groups:
     need = _groups_bytes(rows, groups)
     if need == 0:
         raise ValueError("e0m4_groups_alloc: unsupported size: %d rows, %d groups" % (rows, groups))
     return E0M4Groups(_empty(need // 4, torch.int32, device, stream, "plan"), rows, groups)
+
+
+def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups:
+    """Memory for the layout of `rows` entries by `groups` weights, of zeros: no group has entries until e0m4_groups or e0m4_route has written it."""
+    plan = _new_groups(rows, groups, device, stream)
+    if hasattr(stream, "cuda_stream"):
+        with torch.cuda.stream(stream):
+            plan.data.zero_()
+    else:
+        plan.data.zero_()
+    return plan
 
 
 def _here(where: str, first: torch.Tensor) -> int:
@@ -594,7 +604,7 @@ def e0m4_groups(index: torch.Tensor, groups: int, plan: E0M4Groups = None, strea
     rows, here = index.numel(), _here(where, index)
     _need_here(index, torch.int32, index.shape, "index", here)
     if plan is None:
-        plan = e0m4_groups_alloc(rows, groups, index.device, stream)
+        plan = _new_groups(rows, groups, index.device, stream)
     _check(lib().e0m4_groups(index.data_ptr(), rows, groups, _groups_plan(plan, rows, groups, where, here), _stream(stream)), where)
     return plan
 
@@ -615,7 +625,7 @@ def e0m4_route(logits: torch.Tensor, k: int, scoring: int = E0M4_ROUTE_SOFTMAX, 
         _need_here(count, torch.int32, (1,), "count", here)
     device = logits.device
     if plan is None:
-        plan = e0m4_groups_alloc(tokens * k, experts, device, stream)
+        plan = _new_groups(tokens * k, experts, device, stream)
     pointer = _groups_plan(plan, tokens * k, experts, where, here)
     chosen = _empty((tokens, k), torch.int32, device, stream, "chosen")
     weights = _empty((tokens, k), torch.float32, device, stream, "weights")

@@ -1,0 +1,31 @@
+"""A layout that nothing has written yet holds no entry."""
+import pytest
+import torch
+
+from test_gpu_groups import DEV, e0m4, make_weights  # noqa: F401  (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_new_layout_has_no_entries(e0m4, own_stream):  # noqa: F811
+    rows, groups = 300, 4
+    stream = torch.cuda.Stream() if own_stream else None
+    with torch.cuda.stream(stream):
+        torch.full((1 << 22,), -1, dtype=torch.int32, device=DEV)      # (memory that the allocator may give again)
+    plan = e0m4.e0m4_groups_alloc(rows, groups, DEV, stream=stream)
+    torch.cuda.synchronize()
+    assert plan.offsets.tolist() == [0] * (groups + 1) and not plan.data.any()
+    codes = make_weights(e0m4, "e0m4", groups, 64, 128, 128, 3)[0]
+    x = torch.ones((rows, 128), dtype=torch.float16, device=DEV)
+    for form in range(1, 7):
+        out = torch.full((rows, 64), 5.0, dtype=torch.float16, device=DEV)
+        e0m4.e0m4_set_knob("grouped_form", form)
+        try:
+            e0m4.e0m4_matmul_grouped(x, plan, codes, 64, 128, 128, share=1, out=out)
+        finally:
+            e0m4.e0m4_set_knob("grouped_form", 0)
+        assert (out == 5.0).all()
+    # ... and takes a layout as any other memory does
+    index = torch.arange(rows, dtype=torch.int32, device=DEV) % groups
+    assert torch.equal(e0m4.e0m4_groups(index, groups, plan=plan).order, e0m4.e0m4_groups(index, groups).order)
