@@ -526,7 +526,7 @@ int e0m4_route(const void* logits, int dtype, int64_t tokens, int64_t experts, i
  * (e0m8_codes_bytes) bytes.  N <= 2^24, 0 < K, K as for e0m4_matmul (e0m8_matmul), with
  * share > 0 X of less than 2 GiB, gated the gate's half of a buffer of at most 1 GiB.
  * Accumulation is fp32; every weight is rounded to 16 bits as the dequant entry points do.  Y may not
- * overlap X.  No workspace.  A call is one launch, with work for rows / 128 + min(rows, groups) tiles times
+ * overlap X or the layout.  No workspace.  A call is one launch, with work for rows / 128 + min(rows, groups) tiles times
  * N / 256 (rounded up) blocks of columns, whether tiles are full or not: more than 2^24 - 64 of them do not
  * fit and may be refused (E0M4_ERR_SHAPE).
  */
@@ -541,7 +541,7 @@ int e0m4_bf16_matmul_grouped(const void* X_bf16, int64_t share, const void* plan
  * out[t, n] = base[t, n] + sum_j weights[t, j] * Y[place[t * k + j], n] over the entries j
  * < k that have a place, added up in fp32 in that order and rounded once.  Y is
  * [tokens * k, N] as e0m4_matmul_grouped leaves it, base (NULL: zeros) and out [tokens, N], fp16 or bf16; out may be base, and overlaps
- * nothing else.
+ * nothing else (E0M4_ERR_SHAPE).
  */
 int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, const void* plan, int64_t tokens, int k, int64_t groups, const void* base,
                  void* out, void* stream);
@@ -552,7 +552,8 @@ int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, cons
  * the other rows keep their base.  The layout's entries are the rows, its groups the adapters.  X is [rows, K], base
  * and out [rows, N], rows x_ld, base_ld and out_ld elements apart; A [adapters, rank, K], B [adapters, N, rank], all
  * fp16 or bf16; factors fp32 [adapters] (NULL: ones).  base may be NULL (zeros) or out, with the same distance of rows; otherwise
- * their rows do not overlap (both may be columns of one wider matrix).  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
+ * their rows do not overlap (both may be columns of one wider matrix).  out overlaps neither the layout nor B nor the workspace, from its first row's begin to
+ * its last one's end.  rank is a multiple of 8 from 8 to 128 (adapters of a lower one are padded with zeros), N, K and the
  * distances multiples of 8, N <= 2^24, K <= 2^20, X and one adapter's B less than 2 GiB.  A X is accumulated in fp32 and multiplied
  * with all its bits (fp16: down to 2^-38 of its row's largest), the sum with base is rounded once.  An infinity in A X or B may give NaN.
  * Workspace as for e0m4_matmul.

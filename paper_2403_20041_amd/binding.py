@@ -605,6 +605,8 @@ def e0m4_groups(index: torch.Tensor, groups: int, plan: E0M4Groups = None, strea
     _need_here(index, torch.int32, index.shape, "index", here)
     if plan is None:
         plan = _new_groups(rows, groups, index.device, stream)
+    elif index.data_ptr() < plan.data.data_ptr() + plan.data.numel() * 4 and plan.data.data_ptr() < index.data_ptr() + rows * 4:
+        raise ValueError("e0m4_groups: index must not be a part of the layout that is written")
     _check(lib().e0m4_groups(index.data_ptr(), rows, groups, _groups_plan(plan, rows, groups, where, here), _stream(stream)), where)
     return plan
 

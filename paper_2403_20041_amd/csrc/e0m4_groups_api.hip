@@ -24,6 +24,12 @@ bool rows_overlap(const void* a, int64_t a_ld, const void* b, int64_t b_ld, int6
     return apart < bytes || apart > a_ld - bytes;
 }
 
+// Kernels go where the layout says: results written over one would send those that still read it out of range.
+bool overlaps_plan(const void* p, size_t bytes, const void* plan, int64_t rows, int64_t groups)
+{
+    return overlap(p, bytes, plan, (size_t)plan_words(rows, groups) * 4);
+}
+
 int check_groups(int64_t rows, int64_t groups)
 {
     return rows < 0 || rows > kMaxGroupRows || groups < 1 || groups > kMaxGroups ? E0M4_ERR_SHAPE : E0M4_OK;
@@ -111,7 +117,8 @@ int matmul_grouped(const void* X, int64_t share, const void* plan, int64_t rows,
     if (!X || !plan || !codes || !Y) return E0M4_ERR_NULL;
     if (!aligned(X, 16) || !aligned(plan, 16) || !aligned(codes, 16) || !aligned(Y, 16)) return E0M4_ERR_ALIGN;
     const int64_t n_out = epilogue == E0M4_EPILOGUE_SWIGLU ? N / 2 : N;
-    if (overlap(X, (size_t)(share ? rows / share : rows) * K * 2, Y, (size_t)rows * n_out * 2)) return E0M4_ERR_SHAPE;
+    const size_t y_bytes = (size_t)rows * n_out * 2;
+    if (overlap(X, (size_t)(share ? rows / share : rows) * K * 2, Y, y_bytes) || overlaps_plan(Y, y_bytes, plan, rows, groups)) return E0M4_ERR_SHAPE;
     GroupedArgs a;
     a.X = X;
     a.share = share;
@@ -219,7 +226,9 @@ int e0m4_combine(const void* Y, int dtype, int64_t N, const float* weights, cons
     if (!Y || !weights || !plan || !out) return E0M4_ERR_NULL;
     if (!aligned(Y, 16) || !aligned(weights, 4) || !aligned(plan, 16) || !aligned(base, 16) || !aligned(out, 16)) return E0M4_ERR_ALIGN;
     const size_t bytes = (size_t)tokens * N * 2;
-    if (overlap(out, bytes, Y, bytes * k) || (base && base != out && overlap(out, bytes, base, bytes))) return E0M4_ERR_SHAPE;
+    if (overlap(out, bytes, Y, bytes * k) || (base && base != out && overlap(out, bytes, base, bytes)) || overlap(out, bytes, weights, (size_t)tokens * k * 4) ||
+        overlaps_plan(out, bytes, plan, tokens * k, groups))
+        return E0M4_ERR_SHAPE;
     return launch_combine(Y, N, weights, plan, tokens, k, groups, base, out, dtype, (hipStream_t)stream);
 }
 
@@ -247,7 +256,11 @@ int e0m4_lora(const void* X, int64_t x_ld, int dtype, const void* plan, int64_t 
         return E0M4_ERR_ALIGN;
     if (((rows - 1) * x_ld + K) * 2 > kMaxXBytes) return E0M4_ERR_SHAPE;
     if (base && base != out && rows_overlap(base, base_ld * 2, out, out_ld * 2, rows, N * 2)) return E0M4_ERR_SHAPE;
-    if (workspace_bytes < lora_workspace_bytes(rows, adapters, rank, N, K)) return E0M4_ERR_WORKSPACE;
+    const size_t ws_bytes = lora_workspace_bytes(rows, adapters, rank, N, K), out_bytes = (size_t)((rows - 1) * out_ld + N) * 2;
+    if (overlaps_plan(out, out_bytes, plan, rows, adapters) || overlap(out, out_bytes, workspace, ws_bytes) ||
+        overlap(out, out_bytes, B, (size_t)adapters * N * rank * 2))
+        return E0M4_ERR_SHAPE;
+    if (workspace_bytes < ws_bytes) return E0M4_ERR_WORKSPACE;
     LoraArgs a;
     a.X = X;
     a.x_ld = x_ld;
