@@ -26,9 +26,8 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kFewWaves = 4;
 constexpr int kFewThreads = kFewWaves * 64;
-constexpr int few_weights_ahead(int R) { return R >= 4 ? 2 : R == 2 ? 3 : 4; }      // k blocks of weights that a wavefront has under way
+constexpr int few_weights_ahead(int R) { return R == 4 ? 2 : 3; }       // k blocks of weights that a wavefront has under way (R 2 or 4)
 
-// (as kernel arguments one by one, in registers from the start)
 struct FewArgs {
     const void* X;
     const void* codes;
@@ -54,6 +53,7 @@ __device__ inline void for_each_of(F&& f)
 // depends on the tile that it falls into only by the order of sums.  (The codes' exact values, with scale and bias applied to a group's sums in
 // fp32, would take 28 instead of 60 vector instructions per weight operand and 4 - 6 % less time, bfloat16 6 - 12 %, and be off by half a step of
 // each weight: 35.0 and 33.1 us for 64 tokens with 8 of 128 experts, gated 1536 x 2048.)
+// (Arguments one by one, in registers from the start.)
 template <int FMT, int MT, int R, bool GATED>
 __global__ __launch_bounds__(kFewThreads, 2) void grouped_few_kernel(const char* X, const char* codes, void* Y, const void* plan, int rows, int groups, uint32_t N,
                                                                        uint32_t K, uint32_t chunks, uint32_t kind, uint32_t share_reciprocal)

@@ -33,7 +33,6 @@ constexpr int BK = 64;
 constexpr int kRowBytes = BK * 2, kStages = 4;
 constexpr int TN = 2;                           // operand blocks of 32 weight rows per wavefront
 
-// (as kernel arguments one by one, in registers from the start)
 struct ManyArgs {
     const void* X;
     const void* codes;
@@ -45,7 +44,8 @@ struct ManyArgs {
     uint32_t share, share_reciprocal;           // share 0: rows of X lie in the layout's order
 };
 
-// A tile is 32 TM rows and 64 WN columns; KS groups of WN wavefronts take a part of K each, and their sums are added in LDS.
+// A tile is 32 TM rows and 64 WN columns; KS groups of WN wavefronts take a part of K each, and their sums are added in LDS.  (Arguments one by one, in registers
+// from the start)
 template <int FMT, int G, bool GATED, int TM, int WN, int KS>
 __global__ __launch_bounds__(64 * WN * KS, 2) void grouped_many_kernel(const char* X, const char* codes, void* Y, const void* plan, int rows, int groups,
                                                                                uint32_t N32, uint32_t K32, uint32_t n_tiles, uint32_t share,

@@ -103,7 +103,6 @@ inline int64_t grouped_workgroups(int64_t rows, int64_t groups, int height, int6
     const int64_t n = most_tiles(rows, groups, height) * column_blocks;
     return height < 64 ? n : (n / kNumXcd + kTileClasses) * kNumXcd;
 }
-int64_t grouped_row_block_bytes(const GroupedArgs& a, int format);
 int launch_grouped_few(const GroupedArgs& a, int format, int height, int row_blocks, hipStream_t stream);     // tiles of 16 or 32 rows
 int launch_grouped_many(const GroupedArgs& a, int format, int height, int columns, hipStream_t stream);       // tiles of 64 or 128 rows
 

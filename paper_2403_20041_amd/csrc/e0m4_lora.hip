@@ -468,7 +468,7 @@ int launch_lora(const LoraArgs& a, void* workspace, hipStream_t stream)
     if (p.shrink_tiles * p.splits * kThreadsL > 0xffffffffLL || (p.expand_tiles * p.columns + kCopyWorkgroups) * kThreadsL > 0xffffffffLL) return E0M4_ERR_SHAPE;
     float* H = static_cast<float*>(workspace);
     const int rc = with_sizes(a.dtype == E0M4_BF16, p.shrink_height, a.rank, [&](auto bf, auto mt, auto nt) -> int {
-        if constexpr (decltype(mt)::value > 1 && decltype(nt)::value == 8) return E0M4_ERR_SHAPE;
+        if constexpr (decltype(mt)::value > 1 && decltype(nt)::value != 4) return E0M4_ERR_SHAPE;     // (plan_lora takes them for ranks of 33 to 64 alone)
         else return launch_shrink<decltype(bf)::value, decltype(mt)::value, decltype(nt)::value>(a, p, H, stream);
     });
     if (rc != E0M4_OK) return rc;
