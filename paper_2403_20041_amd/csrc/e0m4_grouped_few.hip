@@ -7,7 +7,7 @@
 // from where the layout's entries say, straight to LDS, whole rows of a k block, and are turned around there into the matrix cores' operands; rows that
 // a tile lacks are requested beyond the buffer's end, which gives zeros without an access to memory.
 // What bounds it: the stream of the used groups' weights, which come once for every tile; X comes from L2 for every R row blocks.  32 tokens with 8 of
-// 128 experts, 2048 x 768 in groups of 64: 20 us, 5 TB/s; 13 with 2 of 8, gated 27392 x 4096 in 8 bits, 904 MB: 121 - 158 us.  One token with 8 of 128, gated
+// 128 experts, 2048 x 768 in groups of 64: 19 us, 5 TB/s; 13 with 2 of 8, gated 27392 x 4096 in 8 bits: 121 us where six of the experts are read, 694 MB, 156 where all are, 926.  One token with 8 of 128, gated
 // 1536 x 2048: 6.0 us of which 2.7 are its bytes' (the tile, its rows, their data and the sums are one chain).  More rows to a tile than 32, and more row
 // blocks than four, were slower throughout (64 rows 66 - 82 us where 16 take 35).
 #include "e0m4_groups.h"
@@ -26,7 +26,9 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kFewWaves = 4;
 constexpr int kFewThreads = kFewWaves * 64;
-constexpr int few_weights_ahead(int R) { return R == 4 ? 2 : 3; }       // k blocks of weights that a wavefront has under way (R 2 or 4)
+// K blocks of weights that a wavefront has under way (R 2 or 4).  One less, these and one more: 64 tokens with 8 of 128 experts, gated 1536 x 2048, 36.0, 36.0 and 38.4 us with
+// 16 rows and R 4, 36.2, 35.6 and 38.0 with R 2, 39.2, 42.4 and 43.1 with 32 rows; 8 with 2 of 8, 14336 x 4096, 38.4, 38.3 and 39.9, 35.5, 35.8 and 38.1, 40.9, 43.3 and 44.2.
+constexpr int few_weights_ahead(int R) { return R == 4 ? 2 : 3; }
 
 struct FewArgs {
     const void* X;

@@ -10,7 +10,7 @@
 //   - one barrier per slice, after sub-step 1.
 // A tile whose group has fewer rows left is computed in as many 32-row blocks as it has, by a loop of its own: with 128 groups of 256 rows on
 // average a third of the tiles are not whole.  Classes of tiles by that number come one after the other (prompt of 1001 tokens with 6 of 64 experts, bfloat16
-// 2816 x 2048, 15 passes: 103 us in the groups' order, 90 by classes).
+// 2816 x 2048: 98 us in the groups' order, 89 by classes; 4096 with 8 of 128, 1536 x 2048, 211 and 207).
 // What bounds it: with whole tiles the clock that the chip holds under matrix instructions (4096 tokens with 2 of 8, 4096 x 13696: 767 - 824 us, 1115 - 1200
 // TFLOP/s, a library's product of 8192^3 on the same card 1078); with short ones the dequantisation, 31 vector instructions a sub-step whatever
 // the rows, which is as long as 96 rows' products take.  Few tiles leave compute units without a workgroup or with a wavefront to a SIMD, which does not fill

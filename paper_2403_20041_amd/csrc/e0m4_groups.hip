@@ -10,8 +10,8 @@
 // integers, an entry's rank among its like within a wavefront comes from ballots over the bits of its group, and wavefronts and workgroups
 // count in order.  Up to 1024 entries are one workgroup's work (choice, counts, places and tiles in one launch), of 64 tokens at most, as many as it
 // chooses for at once; otherwise a first launch chooses and counts per workgroup, and every workgroup of a second one adds up the counts before its own.
-// What bounds it: launches, and the chains of a few hundred dependent instructions in each.  One token of 64 experts 4.6 us, 32 of 128 with 8 chosen 8.9, 128
-// 11.1, 4096 13.8 (6.2 the choice, 7.7 the places).
+// What bounds it: launches, and the chains of a few hundred dependent instructions in each.  One token of 64 experts 4.7 us, 32 of 128 with 8 chosen 8.7, 128
+// 10.9, 4096 13.3 in a graph (traced, the choice 6.3 and the places 7.7).
 #include "e0m4_groups.h"
 
 #include <float.h>
@@ -21,11 +21,17 @@ namespace e0m4 {
 namespace {
 
 constexpr int kWg = 1024;                       // threads of a workgroup that lays entries out
-constexpr int kSmallWg = 256;                   // ... of few tokens by few experts: its barriers are cheaper
+// ... of few tokens by few experts: its barriers are cheaper.  In 256 and 1024 threads one token of 64 experts takes 4.7 and 6.2 us, 16 of 128 with 8 chosen 6.3 and 8.6, as
+// many as it chooses for at once; 60 of 16 with 2 chosen 5.7 and 4.5, 64 of 64 with 4 chosen 9.0 and 5.9.
+constexpr int kSmallWg = 256;
 constexpr int kSmallTokens = 16;
-constexpr int kOneWorkgroupTokens = 64;         // more tokens to choose for, or entries than threads: two launches
+// More tokens to choose for, or entries than threads: two launches.  64 of 64 experts with 4 chosen 5.9 us in one and 9.6 in two, of 128 with 8 chosen 8.9 and 10.3; 128 of
+// them 13.8 and 10.9, 256 of 64 with 4 chosen 12.2 and 10.4 (128 of those 8.0 and 10.0).
+constexpr int kOneWorkgroupTokens = 64;
 constexpr int kCountThreads = 512;
-constexpr int kCountEntries = 256;              // entries of a workgroup of the first of two launches, at least
+// Entries of a workgroup of the first of two launches, at least.  128, 256 and 512: 4096 tokens of 128 experts with 8 chosen 14.8, 13.3 and 16.2 us, 128 of them 11.0, 10.9
+// and 14.2; 256 of 64 with 4 chosen 9.0, 10.4 and 14.0.
+constexpr int kCountEntries = 256;
 
 template <int LANES>
 __device__ inline float lanes_max(float v)

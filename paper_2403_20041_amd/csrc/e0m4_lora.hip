@@ -6,9 +6,10 @@
 // after scaling its row by a power of two), which hold all 24 bits of it: nothing is rounded between the two products.  A wavefront has the rows of
 // the tile and 64 columns at a time, of which a lane holds two runs of 8 of one row.
 // What bounds it: memory, X once, base and out once, A and B of the adapters in use once (and from L2 for every further tile).  3001 rows of five
-// requests, rank 64, 4096 x 4096: 9 - 10 us and 16 - 19 of a floor of 16 together (A comes from L2 94 times, base and out pass through registers of few
-// wavefronts); 8192 rows of rank 16 41 of 41, of rank 64 65 of 42; 5253 rows of rank 16, 15832 x 7672 128 of 84; 64 rows with 40 adapters of rank 16 3.5 and 5.4 us,
-// two launches' chains of loads, of rank 128 30 of 14.
+// requests, rank 64, 4096 x 4096: 9 - 11 us and 16 - 19 of a floor of 16 together (A comes from L2 94 times, base and out pass through registers of few
+// wavefronts, and each step of either launch waits for all that is under way, the second's stores too); 8192 rows of rank 16 42 of 41, of rank 64 71 of 42; 5253 rows of
+// rank 16, 15832 x 7672 126 of 84; 4671 rows of 67 adapters of rank 128, 8008 x 2576 158 of 72; 64 rows with 40 adapters of rank 16 3.7 and 5.7 us, two launches' chains
+// of loads, of rank 128 33 of 15.
 #include "e0m4_groups.h"
 
 #include <algorithm>
@@ -23,7 +24,9 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kWavesL = 4, kThreadsL = kWavesL * 64;
 constexpr int kChunkK = 128;                    // k of a wavefront's turn
-constexpr int64_t kCopyWorkgroups = 256;        // for rows without an adapter
+// For rows without an adapter.  64, 256 and 1024: 43, 15.8 and 11.1 us where none of 3001 rows of 4096 has one, 25.0, 21.5 and 21.7 where one in six has none; 64 rows
+// 4.1 and 7.9 with any.
+constexpr int64_t kCopyWorkgroups = 256;
 constexpr uint32_t kNowhere = 0x80000000u;      // beyond a buffer's end, whatever is added to it
 
 template <bool BF>
@@ -205,7 +208,8 @@ __device__ inline void split_rows(const float* H, bool in, int rank, int splits,
 // MFMAs is column 8 (n/4) + 4 (j%2) + 32 (j/2) + n%4, so that a lane's results, 4 q .. + 3 of each, are the columns 8 q .. + 7 and 32 + 8 q .. + 7 of row n and
 // four lanes read and write 64 bytes of it side by side.  The 64 rows of B are one piece
 // of memory that comes to LDS as it is, but for the order of 16-byte pieces in a row (see order_of): up to a rank of 48 one set of columns ahead; beyond, into the same LDS
-// once its operands are in registers, which leaves room for more workgroups of a compute unit (64 rows of 40 adapters of rank 128: 39 us with two sets, 30 with one).
+// once its operands are in registers, which leaves room for more workgroups of a compute unit (64 rows of 40 adapters of rank 128: 41 us with two sets, 33 with one; 3001
+// rows of rank 64, 4096 x 4096, 38.5 and 31.6, 8192 93 and 71).
 // With more than 16 rows the wavefronts make the operands of 16 rows each and share them through LDS.
 __host__ __device__ constexpr int expand_sets(int NT) { return NT >= 4 ? 1 : 2; }
 __host__ __device__ constexpr int operand_lds(int MT, int NT) { return MT > 1 ? kPartPairs * NT * MT * 1024 + MT * 64 : 0; }
@@ -388,11 +392,12 @@ struct LoraPlan {
 };
 // Tiles of 16 rows for H, of 32 where adapters have many rows of a rank that would be read too often; of 32 for the second launch, of 16 where adapters have
 // no more rows.  3001 rows of five requests, rank 64, 4096 x 4096, both launches, in us (rows of a tile in the first / second launch, splits, workgroups per tile in the
-// second): 16/16 1 4 39.0, 16/32 1 4 30.7, 32/32 2 4 30.5, 32/64 2 4 32.9, 64/32 2 4 33.4, 16/32 1 16 34.3; 512 rows of two, rank 32: 16/16 2 11.7, 16/32 2 11.1, 4 11.5,
-// 8 13.4, 32/32 2 12.4; 64 rows of 40 adapters, rank 16: 1, 2, 4 and 8 splits 9.6, 8.6, 8.4, 9.1; 8192 rows of four, rank 16: 16/32 1 with 2 and 4
-// workgroups per tile 45.4 and 42.5, 32/32 46.5.  Workgroups of the second launch: a rank of 32 or less has little to bring before its first column, and 1024 against 2048
-// took 43.3 and 40.8 (8192 rows of four, rank 16) and 136 and 128 (5253 of one, rank 16, 15832 x 7672); beyond that 448 against 896 took 30 and 35 (3001 rows, rank 64),
-// 98 and 103 (4671 of 67, rank 128, 8008 x 2576), 65 and 63 (8192, rank 64).
+// second): 16/16 1 4 31.0, 16/32 1 4 31.4, 32/32 1 4 33.9, 2 4 31.3, 32/16 2 4 31.9, 16/32 1 16 33.7, 32/32 2 16 35.2; 512 rows of two, rank 32: 16/16 2 12.1,
+// 16/32 2 11.4, 4 11.5, 8 13.5, 32/32 2 12.5; 64 rows of 40 adapters, rank 16: 1, 2, 4 and 8 splits 9.7, 8.6, 8.5, 9.3; 8192 rows of four, rank 16: 16/32 1 with 2, 4 and 8
+// workgroups per tile 45.5, 43.3, 42.0, 32/32 1 8 45.9.  Adapters are counted as if all of them were in use.
+// Workgroups of the second launch: a rank of 32 or less has little to bring before its first column, and 1024 against 2048 take 43.3 and 42.0 (8192 rows of four, rank
+// 16) and 134 and 127 (5253 of one, rank 16, 15832 x 7672).  Beyond that 448, 896 and 2048 take 31.6, 34.6 and 35.5 (3001 rows, rank 64), 32.4, 40.4 and 40.4 (64 rows of
+// 40 adapters, rank 128), 158, 175 and 187 (4671 of 67, rank 128, 8008 x 2576), 84, 96 and 134 (5000 of one, rank 128, 4096 x 4096), and 70.6, 69.1 and 71.9 (8192, rank 64).
 LoraPlan plan_lora(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K)
 {
     LoraPlan p;
