@@ -558,13 +558,13 @@ def _new_groups(rows: int, groups: int, device, stream) -> E0M4Groups:
 
 
 def e0m4_groups_alloc(rows: int, groups: int, device, stream=None) -> E0M4Groups:
-    """Memory for the layout of `rows` entries by `groups` weights, of zeros: no group has entries until e0m4_groups or e0m4_route has written it."""
+    """Memory for the layout of `rows` entries by `groups` weights, of zeros: no group has entries until e0m4_groups or e0m4_route has written it.  The zeros are
+    there when the call returns, for all streams (except in a graph's capture, where they are part of the graph)."""
     plan = _new_groups(rows, groups, device, stream)
-    if hasattr(stream, "cuda_stream"):
-        with torch.cuda.stream(stream):
-            plan.data.zero_()
-    else:
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else None):
         plan.data.zero_()
+        if plan.data.is_cuda and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(plan.data.device).synchronize()
     return plan
 
 

@@ -29,3 +29,38 @@ def test_new_layout_has_no_entries(e0m4, own_stream):  # noqa: F811
     # ... and takes a layout as any other memory does
     index = torch.arange(rows, dtype=torch.int32, device=DEV) % groups
     assert torch.equal(e0m4.e0m4_groups(index, groups, plan=plan).order, e0m4.e0m4_groups(index, groups).order)
+
+
+def test_new_layout_is_ready_on_every_stream(e0m4):  # noqa: F811
+    """Its zeros are there when the call returns, whatever the stream that was current still has to do: they do not come behind what another stream writes."""
+    rows, groups = 300, 4
+    index = torch.arange(rows, dtype=torch.int32, device=DEV) % groups
+    want = e0m4.e0m4_groups(index, groups)
+    a = torch.ones((4096, 4096), device=DEV)
+    side = torch.cuda.Stream()
+    e0m4.e0m4_groups(index, groups, stream=side)       # (loads the kernel)
+    torch.cuda.synchronize()
+    for _ in range(40):
+        b = a @ a                                       # (some milliseconds)
+    plan = e0m4.e0m4_groups_alloc(rows, groups, DEV)
+    e0m4.e0m4_groups(index, groups, plan=plan, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(plan.order, want.order) and torch.equal(plan.offsets, want.offsets) and torch.equal(plan.place, want.place)
+    del b
+
+
+def test_new_layout_in_a_captured_graph(e0m4):  # noqa: F811
+    rows, groups = 300, 4
+    index = torch.arange(rows, dtype=torch.int32, device=DEV) % groups
+    e0m4.e0m4_groups(index, groups)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan = e0m4.e0m4_groups_alloc(rows, groups, DEV)
+        e0m4.e0m4_groups(index, groups, plan=plan)
+    for shift in range(3):
+        index.copy_((torch.arange(rows, device=DEV) + shift) % groups)
+        want = e0m4.e0m4_groups(index, groups)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(plan.order, want.order) and torch.equal(plan.place, want.place)
