@@ -63,7 +63,7 @@ int check_grouped(int64_t rows, int64_t groups, int64_t share, int64_t N, int64_
 // one and full each times a factor of bfloat16's or the 8-bit format's own.  Workgroups are counted as if every row chose a group, at random.
 // The constants are a least-squares fit (logarithm of the ratio to the measurement, rms 10 - 14 %) to 8803 problems, each timed in all forms: 4 to 128
 // groups, 1 to 250 rows to a group, gated and plain, 512 to 27392 columns, 512 to 14080 weights a row, all formats and groups; replays of a graph of 5 or 20 calls on one set of
-// inputs, the least of four (440 of them are in tests/golden/grouped_form_timings.txt).  Choosing by the
+// inputs, the least of four (430 of them are in tests/golden/grouped_form_timings.txt).  Choosing by the
 // estimate costs 1.8 % over the best form of each (geometric mean); without one of the forms 2.1 - 2.5 %, without the second 5.5, without the
 // fourth 8.6.  A seventh, 128 x 256 with two parts of K (10 - 15 % less time where the fourth has a workgroup for every second compute unit), would gain 0.2 %
 // on all.
